@@ -23,6 +23,7 @@ causal softmax attention with the readings listed in the design notes:
 Modules
   codecs           bf16 and OCP fp8-e4m3fn decoding/encoding from their definitions
   paged_attention  page gather/scatter, row-wise and blocked attention
+  layer            step tables, norm with rotation, differential attention
   page_swap        whole-page copies between the page pool and a host block pool
                    (the offloading configuration of Sec. 6.4)
   cachewise_policy the KV-block policy (prefix-aware dispatch, predictive / LRU /
@@ -39,6 +40,7 @@ from .paged_attention import (  # noqa: F401
     gather_sequence_kv,
     write_pages,
 )
+from .layer import diff_attention, norm_rotate, step_tables  # noqa: F401
 from .page_swap import swap_in, swap_out  # noqa: F401
 from . import cachewise_policy  # noqa: F401
 

@@ -26,7 +26,7 @@ tensor on one GPU and contiguous.
 from __future__ import annotations
 
 import ctypes as C
-from typing import Optional
+from typing import NamedTuple, Optional
 
 import numpy as np
 import torch
@@ -37,7 +37,8 @@ __all__ = ["CWError", "init", "pinned_allocations", "arg_plan_calls", "extend_at
            "extend_workspace_bytes", "decode_workspace_bytes", "write_pages_workspace_bytes",
            "set_tuning", "plan_items", "decode_plan", "library", "kv_swap_out", "kv_swap_in", "swap_workspace_bytes",
            "step_attention", "step_workspace_bytes", "check_block_table", "ceiling_mfma_bf16", "ceiling_stream_read",
-           "ceiling_stream_copy"]
+           "ceiling_stream_copy", "build_step_tables", "step_tables_workspace_bytes", "StepTables", "qk_norm_rope",
+           "diff_attention", "diff_workspace_bytes"]
 
 
 class CWError(RuntimeError):
@@ -463,6 +464,172 @@ def check_block_table(block_table, prefix_lens, suffix_lens, num_pages: int, pag
         _dptr(block_table), block_table.shape[1], int(num_pages), _ptr(lp), _ptr(ls), len(lp),
         int(page_size), _dptr(bad), _dptr(workspace), workspace.numel(), _stream()))
     return bad[:len(lp)].cpu().numpy()
+
+
+# around the attention (include/cw_layer.h)
+
+def step_tables_workspace_bytes(num_seqs: int) -> int:
+    return int(library().cw_step_tables_workspace_bytes(int(num_seqs)))
+
+
+class StepTables(NamedTuple):
+    """What build_step_tables wrote besides the block table: cu_rows int32 [B + 1], seq_ids and
+    positions int32 [max_tokens], slots int64 [max_tokens], info int64 [3] (pages taken, new
+    tokens, sequences that need more pages than a table row holds)."""
+    cu_rows: torch.Tensor
+    seq_ids: torch.Tensor
+    positions: torch.Tensor
+    slots: torch.Tensor
+    info: torch.Tensor
+
+
+def build_step_tables(prefix_lens, suffix_lens, free_pages, block_table, page_size: int, max_tokens: int,
+                      cu_rows=None, seq_ids=None, positions=None, slots=None, info=None, workspace=None) -> StepTables:
+    """The step's new block-table entries (in place) and its tokens' index arrays, from int32
+    lengths on the GPU (cw_build_step_tables); waits for nothing."""
+    num, t = len(prefix_lens), int(max_tokens)
+    if t < 0:
+        raise ValueError(f"max_tokens = {t} is negative")
+    i32, i64 = (torch.int32,), (torch.int64,)
+    _want(prefix_lens, "prefix_lens", i32, (num,))
+    _want(suffix_lens, "suffix_lens", i32, (num,))
+    if not isinstance(free_pages, torch.Tensor) or free_pages.dim() != 1 or free_pages.dtype != torch.int32:
+        raise ValueError("free_pages must be a 1-D int32 tensor")
+    if not isinstance(block_table, torch.Tensor) or block_table.dim() != 2 or block_table.dtype != torch.int32:
+        raise ValueError("block_table must be a 2-D int32 tensor [num_seqs, bt_stride]")
+    if block_table.shape[0] < num:
+        raise ValueError(f"block_table has {block_table.shape[0]} rows for {num} sequences")
+    dev = prefix_lens.device
+    new = lambda n, dt: torch.empty(n, dtype=dt, device=dev)
+    cu_rows = new(num + 1, torch.int32) if cu_rows is None else cu_rows
+    seq_ids = new(t, torch.int32) if seq_ids is None else seq_ids
+    positions = new(t, torch.int32) if positions is None else positions
+    slots = new(t, torch.int64) if slots is None else slots
+    info = new(3, torch.int64) if info is None else info
+    _want(cu_rows, "cu_rows", i32, (num + 1,))
+    _want(seq_ids, "seq_ids", i32, (t,))
+    _want(positions, "positions", i32, (t,))
+    _want(slots, "slots", i64, (t,))
+    _want(info, "info", i64, (3,))
+    if workspace is None and (nb := step_tables_workspace_bytes(num)) > 0:
+        workspace = _workspace(nb, dev, None)
+    _one_device(prefix_lens, suffix_lens, free_pages, block_table, cu_rows, seq_ids, positions, slots, info, workspace)
+    _check(library().cw_build_step_tables(
+        _dptr(prefix_lens), _dptr(suffix_lens), num, _dptr(free_pages), free_pages.numel(), int(page_size),
+        _dptr(block_table), block_table.shape[1], t, _dptr(cu_rows), _dptr(seq_ids), _dptr(positions), _dptr(slots),
+        _dptr(info), _dptr(workspace), 0 if workspace is None else workspace.numel(), _stream()))
+    return StepTables(cu_rows, seq_ids, positions, slots, info)
+
+
+def _one_device(*tensors):
+    """Every tensor on the current device, whose stream the call goes to."""
+    devs = {t.device for t in tensors if t is not None}
+    if len(devs) > 1:
+        raise ValueError(f"tensors are on different devices: {sorted(map(str, devs))}")
+    for dev in devs:
+        if dev.type != "cuda":
+            raise ValueError("tensors must be on the GPU")
+        if dev.index != torch.cuda.current_device():
+            raise ValueError(f"tensors are on {dev}, the current device is cuda:{torch.cuda.current_device()}")
+
+
+def _head_rows(t, name, total, heads, d):
+    """Pointer and token stride of a bf16 [T, H, D] tensor whose tokens' heads are contiguous."""
+    _want(t, name, _BF16, (total, heads, d))
+    if not t.is_cuda:
+        raise ValueError("tensors must be on the GPU")
+    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != d):
+        raise ValueError(f"{name}: the heads of a token must be contiguous (strides {t.stride()})")
+    return t.data_ptr(), t.stride(0) if total > 1 else heads * d
+
+
+def qk_norm_rope(q, k, cos_sin, positions, q_weight=None, k_weight=None, eps=1e-6, interleaved=False, v=None,
+                 k_pool=None, v_pool=None, slots=None, k_scale=None, v_scale=None, q_out=None, k_out=None, v_out=None):
+    """Norm of every query and key head, position rotation and (with pools) page write in one
+    pass (cw_qk_norm_rope).  q [T, Hq, D], k, v [T, Hkv, D] may be columns of one projection's
+    output.  Returns (q_out, k_out, v_out), contiguous; v_out is None without v."""
+    if not isinstance(q, torch.Tensor) or q.dim() != 3 or not isinstance(k, torch.Tensor) or k.dim() != 3:
+        raise ValueError("q and k must be 3-D tensors [T, heads, D]")
+    total, hq, d = q.shape
+    hkv = k.shape[1]
+    qp, qs = _head_rows(q, "q", total, hq, d)
+    kp, ks = _head_rows(k, "k", total, hkv, d)
+    vp, vs = (None, 0) if v is None else _head_rows(v, "v", total, hkv, d)
+    f32 = (torch.float32,)
+    if not isinstance(cos_sin, torch.Tensor) or cos_sin.dim() != 2 or cos_sin.dtype != torch.float32:
+        raise ValueError("cos_sin must be a 2-D float32 tensor [positions, rotary_dim]")
+    _want(positions, "positions", (torch.int32,), (total,))
+    for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        if w is not None:
+            _want(w, name, f32, (d,))
+    num_pages, page, dt = 0, 0, L.CW_KV_BF16
+    if k_pool is not None or v_pool is not None:
+        if k_pool is None or v_pool is None or v is None or slots is None:
+            raise ValueError("a page write needs k_pool, v_pool, slots and v")
+        num_pages, pool_heads, page, pool_d = _check_pools(k_pool, v_pool, k_scale, v_scale)
+        if (pool_heads, pool_d) != (hkv, d):
+            raise ValueError(f"pools of {pool_heads} heads of {pool_d} for k of {hkv} heads of {d}")
+        _want(slots, "slots", (torch.int64,), (total,))
+        dt = _kv_dtype(k_pool)
+    elif slots is not None or k_scale is not None or v_scale is not None:
+        raise ValueError("slots, k_scale and v_scale are for a page write (k_pool and v_pool)")
+    new = lambda h: torch.empty(total, h, d, dtype=torch.bfloat16, device=q.device)
+    q_out = new(hq) if q_out is None else q_out
+    k_out = new(hkv) if k_out is None else k_out
+    if v is not None and v_out is None:
+        v_out = new(hkv)
+    _want(q_out, "q_out", _BF16, (total, hq, d))
+    _want(k_out, "k_out", _BF16, (total, hkv, d))
+    if v_out is not None:
+        if v is None:
+            raise ValueError("v_out without v")
+        _want(v_out, "v_out", _BF16, (total, hkv, d))
+    _one_device(q, k, v, cos_sin, positions, q_weight, k_weight, k_pool, v_pool, slots, k_scale, v_scale, q_out, k_out,
+                v_out)
+    _check(library().cw_qk_norm_rope(
+        qp, qs, kp, ks, vp, vs, total, hq, hkv, d, _dptr(q_weight), _dptr(k_weight), float(eps), _dptr(cos_sin),
+        cos_sin.shape[0], cos_sin.shape[1], int(bool(interleaved)), _dptr(positions), _dptr(q_out), _dptr(k_out),
+        _dptr(v_out), _dptr(k_pool), _dptr(v_pool), _dptr(k_scale), _dptr(v_scale), _dptr(slots), num_pages, page, dt,
+        _stream()))
+    return q_out, k_out, v_out
+
+
+def diff_workspace_bytes(prefix_lens, suffix_lens, num_kv_pairs, gqa_group, head_dim, page_size,
+                         kv_dtype="bf16") -> int:
+    lp, ls = _lens_pair(prefix_lens, suffix_lens)
+    return int(library().cw_diff_workspace_bytes(_ptr(lp), _ptr(ls), len(lp), num_kv_pairs, gqa_group, head_dim,
+                                                 page_size, _dtype_code(kv_dtype)))
+
+
+def diff_attention(q, k_new, v_new, k_pool, v_pool, block_table, prefix_lens, suffix_lens, gqa_group, softmax_scale,
+                   lam, k_scale=None, v_scale=None, norm_weight=None, norm_eps=1e-5, out_scale=1.0, out=None,
+                   workspace=None):
+    """Differential attention over the paged cache (cw_diff_attention): q [T, 2 Hp, D], k_new and
+    v_new [T, 2 pairs, D], pools of 2 pairs heads, lam fp32 [Hp], out [T, Hp, 2 D] with Hp = pairs *
+    gqa_group.  The pools are only read."""
+    lp, ls = _lens_pair(prefix_lens, suffix_lens)
+    total = _total(ls)
+    num_pages, heads, page, d = _check_call(q, k_new, v_new, k_pool, v_pool, block_table, len(lp), total, gqa_group,
+                                            k_scale, v_scale)
+    if heads % 2:
+        raise ValueError(f"pools of {heads} heads: differential attention takes pairs of them")
+    hp = heads // 2 * gqa_group
+    _want(lam, "lam", (torch.float32,), (hp,))
+    if norm_weight is not None:
+        _want(norm_weight, "norm_weight", (torch.float32,), (2 * d,))
+    if out is None:
+        out = torch.empty(total, hp, 2 * d, dtype=torch.bfloat16, device=q.device)
+    _want(out, "out", _BF16, (total, hp, 2 * d))
+    _one_device(q, lam, norm_weight, out)
+    if workspace is None:
+        workspace = _workspace(diff_workspace_bytes(lp, ls, heads // 2, gqa_group, d, page, _kv_dtype(k_pool)),
+                               q.device, None)
+    _check(library().cw_diff_attention(
+        _dptr(q), _dptr(k_new), _dptr(v_new), _dptr(k_pool), _dptr(v_pool), _dptr(k_scale), _dptr(v_scale),
+        _dptr(block_table), block_table.shape[1], num_pages, _ptr(lp), _ptr(ls), len(lp), heads // 2, gqa_group, d,
+        page, float(softmax_scale), _kv_dtype(k_pool), _dptr(lam), _dptr(norm_weight), float(norm_eps),
+        float(out_scale), _dptr(out), _dptr(workspace), workspace.numel(), _stream()))
+    return out
 
 
 # measured ceilings (include/cw_ceiling.h): not part of the attention path

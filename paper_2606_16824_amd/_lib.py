@@ -1,5 +1,5 @@
 """ctypes declarations of libcw.so (the C ABI declared in include/cw.h,
-include/cw_ceiling.h and include/cw_policy.h)."""
+include/cw_layer.h, include/cw_ceiling.h and include/cw_policy.h)."""
 from __future__ import annotations
 
 import ctypes as C
@@ -21,6 +21,7 @@ _i32p = C.POINTER(C.c_int32)
 _fp = C.POINTER(C.c_float)
 _vp = C.c_void_p
 _i32 = C.c_int32
+_i64 = C.c_int64
 _sz = C.c_size_t
 
 # name: (restype, argtypes)
@@ -67,6 +68,17 @@ SIGNATURES = {
     "cw_ceiling_mfma_bf16": (C.c_int, [_i32, _i32, _i32, _vp, _vp]),
     "cw_ceiling_stream_read": (C.c_int, [_vp, _sz, _vp, _vp]),
     "cw_ceiling_stream_copy": (C.c_int, [_vp, _vp, _sz, _vp]),
+    # include/cw_layer.h
+    "cw_step_tables_workspace_bytes": (_sz, [_i32]),
+    "cw_build_step_tables": (C.c_int, [_vp, _vp, _i32, _vp, _i32, _i32, _vp, _i32, _i32, _vp, _vp, _vp, _vp, _vp,
+                                       _vp, _sz, _vp]),
+    "cw_qk_norm_rope": (C.c_int, [_vp, _i64, _vp, _i64, _vp, _i64, _i32, _i32, _i32, _i32, _vp, _vp, C.c_float,
+                                  _vp, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32,
+                                  C.c_int, _vp]),
+    "cw_diff_workspace_bytes": (_sz, [_vp, _vp, _i32, _i32, _i32, _i32, _i32, _i32]),
+    "cw_diff_attention": (C.c_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _vp, _vp, _i32, _i32, _i32,
+                                    _i32, _i32, C.c_float, C.c_int, _vp, _vp, C.c_float, C.c_float, _vp, _vp, _sz,
+                                    _vp]),
     # include/cw_policy.h (host-only)
     "cw_policy_simulate": (C.c_int, [_vp, _vp, _vp, _vp, C.c_int64]),
     "cw_policy_predict": (C.c_int, [_vp, _i32, C.c_double, _vp]),

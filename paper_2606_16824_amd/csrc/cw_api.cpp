@@ -9,6 +9,7 @@
 #include <cstdio>
 #include <cstring>
 #include <exception>
+#include <functional>
 #include <initializer_list>
 #include <memory>
 #include <mutex>
@@ -18,6 +19,7 @@
 #include <vector>
 
 #include "../../include/cw.h"
+#include "../../include/cw_layer.h"
 #include "cw_internal.h"
 #include "planner.h"
 
@@ -474,6 +476,14 @@ cw_status_t check_shape(int32_t num_seqs, int32_t num_kv_heads, int32_t gqa_grou
   return CW_OK;
 }
 
+// The shape of a differential attention call: pairs of pool heads.
+cw_status_t check_diff_shape(int32_t num_seqs, int32_t num_pairs, int32_t gqa_group, int32_t head_dim,
+                             int32_t page_size) {
+  if (num_pairs < 1 || num_pairs > 512)
+    return fail(CW_ERR_UNSUPPORTED, "num_kv_pairs = %d (supported: 1..512)", num_pairs);
+  return check_shape(num_seqs, 2 * num_pairs, gqa_group, head_dim, page_size);
+}
+
 // Lengths: non-negative, fit the block table, and the packed sizes fit int32.
 cw_status_t check_lens(const int32_t* lp, const int32_t* ls, int32_t num_seqs, int32_t bt_stride,
                        int32_t page_size, int32_t num_kv_heads, int32_t gqa_group, int32_t head_dim,
@@ -623,8 +633,18 @@ struct StepPlan {
 
 size_t align256h(size_t x) { return (x + 255) & ~size_t(255); }
 
+// How the plans of a step's two sub-batches are made.
+struct PlanKinds {
+  std::function<ExtendPlan(const PlanEnv&, const int32_t* lp, const int32_t* ls, int32_t num_seqs, const int32_t* cu_rows,
+                           const int32_t* bt_rows)>
+      extend;
+  std::function<ExtendPlan(const PlanEnv&, const int32_t* lp, int32_t num_seqs, size_t meta_at, const int32_t* cu_rows,
+                           const int32_t* bt_rows)>
+      decode;
+};
+
 StepPlan make_step_plan(const PlanEnv& env, const int32_t* lp, const int32_t* ls, int32_t num_seqs,
-                        int32_t num_kv_heads, int32_t gqa_group, int32_t head_dim, int32_t page_size, cw_kv_dtype_t kv_dtype) {
+                        const PlanKinds& kinds) {
   StepPlan sp;
   std::vector<int32_t> lp_e, ls_e, cu_e, lp_d, cu_d;
   int32_t cu = 0;
@@ -643,14 +663,13 @@ StepPlan make_step_plan(const PlanEnv& env, const int32_t* lp, const int32_t* ls
     cu += ls[b];
   }
   if (!sp.ext.empty())
-    sp.ext_plan = make_plan(env, lp_e.data(), ls_e.data(), static_cast<int32_t>(sp.ext.size()), num_kv_heads,
-                            gqa_group, head_dim, cu_e.data(), sp.ext.data());
+    sp.ext_plan = kinds.extend(env, lp_e.data(), ls_e.data(), static_cast<int32_t>(sp.ext.size()), cu_e.data(),
+                               sp.ext.data());
   sp.off_ext_meta = align256h(sp.seqs.size() * sizeof(SeqInfo));
   sp.off_dec_meta = sp.off_ext_meta + sp.ext_plan.meta_bytes;
   if (!sp.dec.empty())
-    sp.dec_plan = make_decode_plan(env, lp_d.data(), static_cast<int32_t>(sp.dec.size()), num_kv_heads,
-                                   gqa_group, head_dim, page_size, kv_dtype, sp.off_dec_meta, cu_d.data(),
-                                   sp.dec.data());
+    sp.dec_plan = kinds.decode(env, lp_d.data(), static_cast<int32_t>(sp.dec.size()), sp.off_dec_meta, cu_d.data(),
+                               sp.dec.data());
   sp.meta_bytes = sp.off_dec_meta + sp.dec_plan.meta_bytes;
   sp.off_ext_part = sp.meta_bytes;
   sp.off_dec_part = sp.off_ext_part + (sp.ext_plan.total_bytes - sp.ext_plan.meta_bytes);
@@ -658,17 +677,43 @@ StepPlan make_step_plan(const PlanEnv& env, const int32_t* lp, const int32_t* ls
   return sp;
 }
 
+size_t step_kept_bytes(const StepPlan& p) {
+  return kept_bytes(p.ext_plan) + kept_bytes(p.dec_plan) + p.seqs.size() * 24;
+}
+
 std::shared_ptr<const StepPlan> step_plan(const int32_t* lp, const int32_t* ls, int32_t num_seqs,
                                           int32_t num_kv_heads, int32_t gqa_group, int32_t head_dim,
                                           int32_t page_size, cw_kv_dtype_t kv_dtype) {
   thread_local LastPlan<StepPlan> last;
+  const PlanKinds kinds{
+      [&](const PlanEnv& env, const int32_t* lp_e, const int32_t* ls_e, int32_t n, const int32_t* cu, const int32_t* bt) {
+        return make_plan(env, lp_e, ls_e, n, num_kv_heads, gqa_group, head_dim, cu, bt);
+      },
+      [&](const PlanEnv& env, const int32_t* lp_d, int32_t n, size_t meta_at, const int32_t* cu, const int32_t* bt) {
+        return make_decode_plan(env, lp_d, n, num_kv_heads, gqa_group, head_dim, page_size, kv_dtype, meta_at, cu, bt);
+      }};
   return last.get(lp, ls, num_seqs, {num_kv_heads, gqa_group, head_dim, page_size, int32_t(kv_dtype)},
-                  [&](const PlanEnv& env) {
-                    return make_step_plan(env, lp, ls, num_seqs, num_kv_heads, gqa_group, head_dim, page_size, kv_dtype);
-                  },
-                  [](const StepPlan& p) {
-                    return kept_bytes(p.ext_plan) + kept_bytes(p.dec_plan) + p.seqs.size() * 24;
-                  });
+                  [&](const PlanEnv& env) { return make_step_plan(env, lp, ls, num_seqs, kinds); }, step_kept_bytes);
+}
+
+// The plan of a differential attention call: like a step's, of its key pairs, with the
+// row block and tile of those kernels and two maps of 2 head_dim values per row.
+std::shared_ptr<const StepPlan> diff_plan(const int32_t* lp, const int32_t* ls, int32_t num_seqs, int32_t num_pairs,
+                                          int32_t gqa_group, int32_t head_dim, int32_t page_size,
+                                          cw_kv_dtype_t kv_dtype) {
+  thread_local LastPlan<StepPlan> last;
+  const bool fp8 = kv_dtype == CW_KV_FP8_E4M3FN;
+  const PlanKinds kinds{
+      [&](const PlanEnv& env, const int32_t* lp_e, const int32_t* ls_e, int32_t n, const int32_t* cu, const int32_t* bt) {
+        return build_extend_plan(lp_e, ls_e, n, num_pairs, gqa_group, 2 * head_dim, DIFF_BLOCK_M, 1, env.cus, env.xcds,
+                                 env.tuning, cu, bt, 2);
+      },
+      [&](const PlanEnv& env, const int32_t* lp_d, int32_t n, size_t meta_at, const int32_t* cu, const int32_t* bt) {
+        return build_decode_plan(lp_d, n, num_pairs, gqa_group, 2 * head_dim, page_size, diff_decode_keys_per_tile(),
+                                 diff_decode_waves_per_cu(head_dim, fp8), env.cus, env.tuning, meta_at, cu, bt, 2);
+      }};
+  return last.get(lp, ls, num_seqs, {num_pairs, gqa_group, head_dim, page_size, int32_t(kv_dtype)},
+                  [&](const PlanEnv& env) { return make_step_plan(env, lp, ls, num_seqs, kinds); }, step_kept_bytes);
 }
 
 // Kernel arguments of a plan whose meta is read at `meta` and whose partials
@@ -1038,6 +1083,124 @@ cw_status_t step_impl(const void* q, const void* k_new, const void* v_new, void*
   }, arg_plan);
 }
 
+cw_status_t diff_impl(const void* q, const void* k_new, const void* v_new, const void* k_pool, const void* v_pool,
+                      const float* k_scale, const float* v_scale, const int32_t* block_table, int32_t bt_stride,
+                      int32_t num_pages, const int32_t* lp, const int32_t* ls, int32_t num_seqs, int32_t num_pairs,
+                      int32_t gqa_group, int32_t head_dim, int32_t page_size, float softmax_scale,
+                      cw_kv_dtype_t kv_dtype, const float* lam, const float* norm_weight, float norm_eps,
+                      float out_scale, void* out, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  cw_status_t s = check_diff_shape(num_seqs, num_pairs, gqa_group, head_dim, page_size);
+  if (s != CW_OK) return s;
+  s = check_dtype(kv_dtype, k_scale, v_scale);
+  if (s != CW_OK) return s;
+  if (!(softmax_scale > 0.0f) || !std::isfinite(softmax_scale))
+    return fail(CW_ERR_UNSUPPORTED, "softmax_scale = %g (must be finite and > 0)", double(softmax_scale));
+  if (!std::isfinite(out_scale) || (norm_weight && (!(norm_eps >= 0.f) || !std::isfinite(norm_eps))))
+    return fail(CW_ERR_UNSUPPORTED, "out_scale = %g, norm_eps = %g (must be finite, norm_eps >= 0)", double(out_scale),
+                double(norm_eps));
+  if (num_pages < 0) return fail(CW_ERR_BAD_LENS, "num_pages = %d is negative", num_pages);
+  // rows of 2 gqa_group query heads per key pair, as wide as two pool heads' values
+  s = check_lens(lp, ls, num_seqs, bt_stride, page_size, 2 * num_pairs, gqa_group, head_dim, true);
+  if (s != CW_OK) return s;
+  const int64_t total = sum_suffix(ls, num_seqs);
+  if (total == 0) return CW_OK;
+  if (!q || !k_new || !v_new || !out || !block_table || !lam)
+    return fail(CW_ERR_NULL, "q, k_new, v_new, lam, out and block_table are required");
+  bool any_prefix = false;
+  for (int32_t b = 0; b < num_seqs; ++b) any_prefix |= lp[b] > 0 && ls[b] > 0;
+  if (any_prefix && (!k_pool || !v_pool)) return fail(CW_ERR_NULL, "k_pool / v_pool is NULL");
+  if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(out) || !aligned16(k_pool) ||
+      !aligned16(v_pool) || !aligned16(norm_weight) || !aligned16(workspace))
+    return fail(CW_ERR_ALIGN, "tensor and workspace pointers must be 16-byte aligned");
+  if ((reinterpret_cast<uintptr_t>(block_table) | reinterpret_cast<uintptr_t>(lam) |
+       reinterpret_cast<uintptr_t>(k_scale) | reinterpret_cast<uintptr_t>(v_scale)) & 3u)
+    return fail(CW_ERR_ALIGN, "block_table, lam and scales must be 4-byte aligned");
+
+  const std::shared_ptr<const StepPlan> kept =
+      diff_plan(lp, ls, num_seqs, num_pairs, gqa_group, head_dim, page_size, kv_dtype);
+  const StepPlan& sp = *kept;
+  if (workspace == nullptr || workspace_bytes < sp.total_bytes)
+    return fail(CW_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", workspace_bytes, sp.total_bytes);
+  const size_t rows_q = size_t(total) * num_pairs * gqa_group * 2 * head_dim * 2;  // of q and of out
+  s = check_attention_alias(q, k_new, v_new, k_pool, v_pool, k_scale, v_scale, block_table, bt_stride, num_pages,
+                            num_seqs, 2 * num_pairs, gqa_group, head_dim, page_size, kv_dtype, total, out, nullptr,
+                            workspace, workspace_bytes);
+  if (s != CW_OK) return s;
+  s = check_no_alias({{out, rows_q, "out"}},
+                     {{lam, size_t(num_pairs) * gqa_group * 4, "lam"},
+                      {norm_weight, size_t(head_dim) * 8, "norm_weight"}});
+  if (s != CW_OK) return s;
+
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  auto params = [&](const ExtendPlan& plan, const uint8_t* meta, size_t part) {
+    DiffParams dp{};
+    dp.a = plan_params(plan, meta, ws, part);
+    dp.a.q = q;
+    dp.a.k_new = k_new;
+    dp.a.v_new = v_new;
+    dp.a.k_pool = k_pool;
+    dp.a.v_pool = v_pool;
+    dp.a.k_scale = k_scale;
+    dp.a.v_scale = v_scale;
+    dp.a.block_table = block_table;
+    dp.a.out = out;
+    dp.a.bt_stride = bt_stride;
+    dp.a.num_kv_heads = num_pairs;
+    dp.a.gqa_group = gqa_group;
+    dp.a.num_seqs = num_seqs;
+    dp.a.scale_log2 = softmax_scale * 1.4426950408889634f;
+    dp.lam = lam;
+    dp.weight = norm_weight;
+    dp.eps = norm_eps;
+    dp.out_scale = out_scale;
+    return dp;
+  };
+  const bool fp8 = kv_dtype == CW_KV_FP8_E4M3FN;
+  CompactUpload cu;
+  const bool compact = !sp.dec.empty() && compact_upload(sp.dec_plan, sp.off_dec_meta, &cu);
+  auto launch = [&](const uint8_t* meta, const ArgPlanBuf* ap) -> cw_status_t {
+    hipError_t e = hipSuccess;
+    if (!sp.dec.empty()) {
+      DiffParams pd = params(sp.dec_plan, ap != nullptr ? nullptr : meta + sp.off_dec_meta, sp.off_dec_part);
+      if (ap != nullptr) {
+        pd.a.ap_seqs = static_cast<int32_t>(sp.off_dec_meta + sp.dec_plan.off_seqs);
+        pd.a.ap_desc = static_cast<int32_t>(cu.bytes);
+      }
+      if ((e = launch_diff_decode(pd, head_dim, page_size, fp8, stream, ap)) != hipSuccess)
+        return hip_fail(e, "diff decode kernel launch");
+      if ((e = launch_diff_combine(pd, head_dim, sp.dec_plan.max_parts, stream, ap)) != hipSuccess)
+        return hip_fail(e, "diff combine kernel launch");
+    }
+    if (!sp.ext.empty()) {
+      DiffParams pe = params(sp.ext_plan, ap != nullptr ? nullptr : meta + sp.off_ext_meta, sp.off_ext_part);
+      if (ap != nullptr) {
+        pe.a.ap_seqs = static_cast<int32_t>(sp.off_ext_meta + sp.ext_plan.off_seqs);
+        pe.a.ap_items = static_cast<int32_t>(sp.off_ext_meta + sp.ext_plan.off_items);
+        pe.a.ap_groups = static_cast<int32_t>(sp.off_ext_meta + sp.ext_plan.off_groups);
+      }
+      if ((e = launch_diff_extend(pe, head_dim, page_size, fp8, stream, ap)) != hipSuccess)
+        return hip_fail(e, "diff extend kernel launch");
+      if ((e = launch_diff_combine(pe, head_dim, sp.ext_plan.max_parts, stream, ap)) != hipSuccess)
+        return hip_fail(e, "diff combine kernel launch");
+    }
+    return CW_OK;
+  };
+  auto head = [&](uint8_t* h) {
+    std::fill(h, h + sp.off_ext_meta, uint8_t(0));
+    if (!sp.ext.empty()) pack_plan_meta(sp.ext_plan, h + sp.off_ext_meta);
+  };
+  const bool arg_plan =
+      arg_plans() && (sp.dec.empty() || (sp.ext.empty() && compact && compact_arg_fits(cu.bytes)));
+  const size_t whole_bytes = sp.off_ext_meta + sp.ext_plan.whole_meta_bytes + sp.dec_plan.whole_meta_bytes;
+  return stage_and_launch(sp.meta_bytes, whole_bytes, ws, stream, [&](uint8_t* h) {
+    head(h);
+    if (!sp.dec.empty()) pack_plan_meta(sp.dec_plan, h + sp.off_dec_meta);
+  }, launch, false, plan_direct(false), compact ? &cu : nullptr, [&](uint8_t* h) {
+    head(h);
+    pack_plan_head(sp.dec_plan, h + sp.off_dec_meta);
+  }, arg_plan);
+}
+
 // Runs an entry point's body: a failed host allocation (or any other C++
 // exception) becomes a status, so nothing is thrown across the C ABI.
 template <class F>
@@ -1195,6 +1358,210 @@ cw_status_t cw_kv_write_pages(const void* k_new, const void* v_new, void* k_pool
       return e == hipSuccess ? CW_OK : hip_fail(e, "write_pages kernel launch");
     };
     return stage_and_launch(bytes, bytes, workspace, stream, fill, launch, false, false, nullptr, fill, in_args);
+  });
+}
+
+size_t cw_step_tables_workspace_bytes(int32_t num_seqs) {
+  if (num_seqs <= kStepTablesLdsSeqs) return 0;
+  return align256h(2 * (size_t(num_seqs) + 1) * sizeof(int32_t));
+}
+
+cw_status_t cw_build_step_tables(const int32_t* prefix_lens, const int32_t* suffix_lens,
+                                 int32_t num_seqs, const int32_t* free_pages, int32_t num_free,
+                                 int32_t page_size, int32_t* block_table, int32_t bt_stride,
+                                 int32_t max_tokens, int32_t* cu_rows, int32_t* seq_ids,
+                                 int32_t* positions, int64_t* slots, int64_t* info,
+                                 void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  return guarded([&]() -> cw_status_t {
+    if (page_size != 16 && page_size != 64)
+      return fail(CW_ERR_UNSUPPORTED, "page_size = %d (supported: 16, 64)", page_size);
+    if (num_seqs < 0 || num_free < 0 || max_tokens < 0)
+      return fail(CW_ERR_BAD_LENS, "negative count (num_seqs = %d, num_free = %d, max_tokens = %d)", num_seqs, num_free,
+                  max_tokens);
+    if (num_seqs > 0 && bt_stride < 1) return fail(CW_ERR_BAD_LENS, "bt_stride = %d must be >= 1", bt_stride);
+    if (num_seqs > 0 && (!prefix_lens || !suffix_lens || !block_table))
+      return fail(CW_ERR_NULL, "prefix_lens, suffix_lens and block_table are required");
+    if (num_free > 0 && !free_pages) return fail(CW_ERR_NULL, "free_pages is NULL with num_free = %d", num_free);
+    const uintptr_t four = reinterpret_cast<uintptr_t>(prefix_lens) | reinterpret_cast<uintptr_t>(suffix_lens) |
+                           reinterpret_cast<uintptr_t>(free_pages) | reinterpret_cast<uintptr_t>(block_table) |
+                           reinterpret_cast<uintptr_t>(cu_rows) | reinterpret_cast<uintptr_t>(seq_ids) |
+                           reinterpret_cast<uintptr_t>(positions);
+    const uintptr_t eight = reinterpret_cast<uintptr_t>(slots) | reinterpret_cast<uintptr_t>(info);
+    if ((four & 3u) || (eight & 7u))
+      return fail(CW_ERR_ALIGN, "int32 arrays must be 4-byte and int64 arrays 8-byte aligned");
+    const size_t need = cw_step_tables_workspace_bytes(num_seqs);
+    if (need > 0 && (workspace == nullptr || workspace_bytes < need))
+      return fail(CW_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
+    if (need > 0 && !aligned16(workspace)) return fail(CW_ERR_ALIGN, "workspace must be 16-byte aligned");
+    const size_t n = size_t(num_seqs), t = size_t(max_tokens);
+    const cw_status_t s = check_no_alias(
+        {{block_table, n * bt_stride * 4, "block_table"}, {cu_rows, (n + 1) * 4, "cu_rows"}, {seq_ids, t * 4, "seq_ids"},
+         {positions, t * 4, "positions"}, {slots, t * 8, "slots"}, {info, 24, "info"}, {workspace, need, "workspace"}},
+        {{prefix_lens, n * 4, "prefix_lens"}, {suffix_lens, n * 4, "suffix_lens"},
+         {free_pages, size_t(num_free) * 4, "free_pages"}});
+    if (s != CW_OK) return s;
+    StepTablesParams p{};
+    p.prefix_lens = prefix_lens;
+    p.suffix_lens = suffix_lens;
+    p.free_pages = free_pages;
+    p.block_table = block_table;
+    p.cu_rows = cu_rows;
+    p.seq_ids = seq_ids;
+    p.positions = positions;
+    p.slots = slots;
+    p.info = info;
+    p.sums = static_cast<int32_t*>(workspace);
+    p.num_seqs = num_seqs;
+    p.num_free = num_free;
+    p.page_size = page_size;
+    p.bt_stride = bt_stride;
+    p.max_tokens = max_tokens;
+    const hipError_t e = launch_step_tables(p, stream);
+    return e == hipSuccess ? CW_OK : hip_fail(e, "step_tables kernel launch");
+  });
+}
+
+cw_status_t cw_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                            const void* v, int64_t v_stride, int32_t num_tokens,
+                            int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                            const float* q_weight, const float* k_weight, float eps,
+                            const float* cos_sin, int32_t num_positions, int32_t rotary_dim,
+                            int32_t interleaved, const int32_t* positions, void* q_out,
+                            void* k_out, void* v_out, void* k_pool, void* v_pool,
+                            const float* k_scale, const float* v_scale, const int64_t* slots,
+                            int32_t num_pages, int32_t page_size, cw_kv_dtype_t kv_dtype,
+                            hipStream_t stream) {
+  return guarded([&]() -> cw_status_t {
+    const bool pools = k_pool != nullptr || v_pool != nullptr;
+    cw_status_t s = check_shape(0, num_kv_heads, 1, head_dim, pools ? page_size : 16);
+    if (s != CW_OK) return s;
+    if (num_q_heads < 1 || num_q_heads > 16384)
+      return fail(CW_ERR_UNSUPPORTED, "num_q_heads = %d (supported: 1..16384)", num_q_heads);
+    if (rotary_dim < 16 || rotary_dim > head_dim || rotary_dim % 16 != 0)
+      return fail(CW_ERR_UNSUPPORTED, "rotary_dim = %d (supported: multiples of 16 in 16..head_dim)", rotary_dim);
+    if (!(eps >= 0.f) || !std::isfinite(eps))
+      return fail(CW_ERR_UNSUPPORTED, "eps = %g (must be finite and >= 0)", double(eps));
+    if (num_tokens < 0 || num_tokens > INT32_MAX / 32 || num_positions < 0 || num_pages < 0)
+      return fail(CW_ERR_BAD_LENS, "count out of range (num_tokens = %d, num_positions = %d, num_pages = %d)", num_tokens,
+                  num_positions, num_pages);
+    if (pools) {
+      s = check_dtype(kv_dtype, k_scale, v_scale);
+      if (s != CW_OK) return s;
+    }
+    if (num_tokens == 0) return CW_OK;
+    if (!q || !k || !q_out || !k_out || !cos_sin || !positions)
+      return fail(CW_ERR_NULL, "q, k, q_out, k_out, cos_sin and positions are required");
+    if (pools && (!k_pool || !v_pool || !slots || !v))
+      return fail(CW_ERR_NULL, "a page write needs k_pool, v_pool, slots and v");
+    if (v_out && !v) return fail(CW_ERR_NULL, "v_out without v");
+    const int64_t q_row = int64_t(num_q_heads) * head_dim, kv_row = int64_t(num_kv_heads) * head_dim;
+    auto bad_stride = [&](const void* x, int64_t stride, int64_t row) {
+      return x != nullptr && (stride % 8 != 0 || (num_tokens > 1 && stride < row) || stride > (int64_t(1) << 31));
+    };
+    if (bad_stride(q, q_stride, q_row) || bad_stride(k, k_stride, kv_row) || bad_stride(v, v_stride, kv_row))
+      return fail(CW_ERR_ALIGN, "token strides must be multiples of 8 elements and hold a token's heads");
+    for (const void* x : {q, k, v, static_cast<const void*>(q_weight), static_cast<const void*>(k_weight),
+                          static_cast<const void*>(cos_sin), static_cast<const void*>(q_out),
+                          static_cast<const void*>(k_out), static_cast<const void*>(v_out),
+                          static_cast<const void*>(k_pool), static_cast<const void*>(v_pool)})
+      if (!aligned16(x)) return fail(CW_ERR_ALIGN, "tensor pointers must be 16-byte aligned");
+    if ((reinterpret_cast<uintptr_t>(positions) & 3u) || (reinterpret_cast<uintptr_t>(slots) & 7u) ||
+        ((reinterpret_cast<uintptr_t>(k_scale) | reinterpret_cast<uintptr_t>(v_scale)) & 3u))
+      return fail(CW_ERR_ALIGN, "positions must be 4-byte, slots 8-byte and scales 4-byte aligned");
+    // an output may be its own contiguous input; the inputs between the first and the last
+    // token's heads may hold other columns of a projection's output
+    auto span_in = [&](const void* x, int64_t stride, int64_t row) {
+      return (size_t(num_tokens - 1) * size_t(num_tokens > 1 ? stride : 0) + size_t(row)) * 2;
+    };
+    auto in_place = [&](const void* x, int64_t stride, int64_t row, const void* y) {
+      return x == y && (stride == row || num_tokens == 1);
+    };
+    const bool fp8 = pools && kv_dtype == CW_KV_FP8_E4M3FN;
+    const size_t out_q = size_t(num_tokens) * q_row * 2, out_kv = size_t(num_tokens) * kv_row * 2;
+    const size_t pool = pools ? size_t(num_pages) * kv_row * page_size * (fp8 ? 1 : 2) : 0;
+    const size_t scales = fp8 ? size_t(num_pages) * num_kv_heads * 4 : 0;
+    s = check_no_alias(
+        {{q_out, out_q, "q_out"}, {k_out, out_kv, "k_out"}, {v_out, out_kv, "v_out"}, {k_pool, pool, "k_pool"},
+         {v_pool, pool, "v_pool"}},
+        {{q_weight, size_t(head_dim) * 4, "q_weight"}, {k_weight, size_t(head_dim) * 4, "k_weight"},
+         {cos_sin, size_t(num_positions) * rotary_dim * 4, "cos_sin"}, {positions, size_t(num_tokens) * 4, "positions"},
+         {slots, pools ? size_t(num_tokens) * 8 : 0, "slots"}, {k_scale, scales, "k_scale"}, {v_scale, scales, "v_scale"}});
+    if (s != CW_OK) return s;
+    const Span in_q{q, span_in(q, q_stride, q_row), "q"}, in_k{k, span_in(k, k_stride, kv_row), "k"},
+        in_v{v, v ? span_in(v, v_stride, kv_row) : 0, "v"};
+    struct Out {
+      Span span;
+      const Span* own;  // the input that it may be, and whether it is
+      bool same;
+    };
+    const Out outs[] = {{{q_out, out_q, "q_out"}, &in_q, in_place(q, q_stride, q_row, q_out)},
+                        {{k_out, out_kv, "k_out"}, &in_k, in_place(k, k_stride, kv_row, k_out)},
+                        {{v_out, out_kv, "v_out"}, &in_v, in_place(v, v_stride, kv_row, v_out)},
+                        {{k_pool, pool, "k_pool"}, nullptr, false},
+                        {{v_pool, pool, "v_pool"}, nullptr, false}};
+    for (const Out& o : outs)
+      for (const Span* i : {&in_q, &in_k, &in_v})
+        if (!(o.same && i == o.own) && overlap(o.span, *i))
+          return fail(CW_ERR_ALIAS, "%s overlaps %s", o.span.name, i->name);
+    NormRopeParams p{};
+    p.q = q;
+    p.k = k;
+    p.v = v_out || pools ? v : nullptr;
+    p.q_weight = q_weight;
+    p.k_weight = k_weight;
+    p.cos_sin = cos_sin;
+    p.positions = positions;
+    p.slots = slots;
+    p.q_out = q_out;
+    p.k_out = k_out;
+    p.v_out = v_out;
+    p.k_pool = k_pool;
+    p.v_pool = v_pool;
+    p.k_scale = k_scale;
+    p.v_scale = v_scale;
+    p.q_stride = q_stride;
+    p.k_stride = k_stride;
+    p.v_stride = v_stride;
+    p.eps = eps;
+    p.num_tokens = num_tokens;
+    p.hq = num_q_heads;
+    p.hkv = num_kv_heads;
+    p.num_positions = num_positions;
+    p.rot = rotary_dim;
+    p.num_pages = num_pages;
+    p.page_size = page_size;
+    const hipError_t e = launch_qk_norm_rope(p, head_dim, interleaved != 0, !pools ? 0 : fp8 ? 2 : 1, stream);
+    return e == hipSuccess ? CW_OK : hip_fail(e, "qk_norm_rope kernel launch");
+  });
+}
+
+size_t cw_diff_workspace_bytes(const int32_t* prefix_lens_h, const int32_t* suffix_lens_h, int32_t num_seqs,
+                               int32_t num_kv_pairs, int32_t gqa_group, int32_t head_dim, int32_t page_size,
+                               cw_kv_dtype_t kv_dtype) {
+  return guarded_value<size_t>(0, [&]() -> size_t {
+    if (check_diff_shape(num_seqs, num_kv_pairs, gqa_group, head_dim, page_size) != CW_OK) return 0;
+    if (kv_dtype != CW_KV_BF16 && kv_dtype != CW_KV_FP8_E4M3FN) return 0;
+    if (check_lens(prefix_lens_h, suffix_lens_h, num_seqs, 0, page_size, 2 * num_kv_pairs, gqa_group, head_dim,
+                   false) != CW_OK)
+      return 0;
+    return diff_plan(prefix_lens_h, suffix_lens_h, num_seqs, num_kv_pairs, gqa_group, head_dim, page_size, kv_dtype)
+        ->total_bytes;
+  });
+}
+
+cw_status_t cw_diff_attention(const void* q, const void* k_new, const void* v_new, const void* k_pool,
+                              const void* v_pool, const float* k_scale, const float* v_scale,
+                              const int32_t* block_table, int32_t bt_stride, int32_t num_pages,
+                              const int32_t* prefix_lens_h, const int32_t* suffix_lens_h, int32_t num_seqs,
+                              int32_t num_kv_pairs, int32_t gqa_group, int32_t head_dim, int32_t page_size,
+                              float softmax_scale, cw_kv_dtype_t kv_dtype, const float* lam,
+                              const float* norm_weight, float norm_eps, float out_scale, void* out,
+                              void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  return guarded([&]() -> cw_status_t {
+    return diff_impl(q, k_new, v_new, k_pool, v_pool, k_scale, v_scale, block_table, bt_stride, num_pages,
+                     prefix_lens_h, suffix_lens_h, num_seqs, num_kv_pairs, gqa_group, head_dim, page_size,
+                     softmax_scale, kv_dtype, lam, norm_weight, norm_eps, out_scale, out, workspace,
+                     workspace_bytes, stream);
   });
 }
 

@@ -140,6 +140,18 @@ struct ExtendParams {
 };
 
 
+// Differential attention: `a` as for the extend and decode kernels, with num_kv_heads the
+// key pairs, gqa_group the query pairs of each, part_rows twice a plan's rows (the first
+// map's, then the second map's; part_o is [n_parts, part_rows, 2 D] fp32) and no lse.
+struct DiffParams {
+  ExtendParams a;
+  const float* lam;     // [query pairs]
+  const float* weight;  // [2 D] or nullptr: no norm
+  float eps;
+  float out_scale;
+};
+constexpr int DIFF_BLOCK_M = 128;  // packed query rows of a diff extend work item
+
 // Whole-block copies between two block pools (device page pool <-> host block
 // pool): block src_ids[i] of (src_k, src_v) goes to block dst_ids[i] of
 // (dst_k, dst_v); scales (fp8 pools) likewise, `scales_per_block` floats each.
@@ -157,6 +169,54 @@ struct SwapParams {
   int32_t n;
   int32_t block_bytes;  // Hkv * P * D * element bytes, a multiple of 16
   int32_t scales_per_block;  // Hkv
+};
+
+// Tables of a serving step, from lengths on the device (step_tables.hip).
+constexpr int kStepTablesLdsSeqs = 4096;  // up to here one launch, every workgroup summing the lengths itself
+struct StepTablesParams {
+  const int32_t* prefix_lens;  // [num_seqs], device
+  const int32_t* suffix_lens;
+  const int32_t* free_pages;  // [num_free]
+  int32_t* block_table;       // [num_seqs, bt_stride]
+  int32_t* cu_rows;           // [num_seqs + 1] or nullptr
+  int32_t* seq_ids;           // [max_tokens] or nullptr
+  int32_t* positions;         // [max_tokens] or nullptr
+  int64_t* slots;             // [max_tokens] or nullptr
+  int64_t* info;              // [3] or nullptr: pages taken, new tokens, sequences longer than a table row
+  int32_t* sums;              // workspace, 2 (num_seqs + 1), above kStepTablesLdsSeqs sequences
+  int32_t num_seqs;
+  int32_t num_free;
+  int32_t page_size;
+  int32_t bt_stride;
+  int32_t max_tokens;
+};
+
+// Norm, rotation and page write of new tokens (qk_norm_rope.hip).
+struct NormRopeParams {
+  const void* q;
+  const void* k;
+  const void* v;  // nullptr: none
+  const float* q_weight;  // [D] or nullptr: no norm
+  const float* k_weight;
+  const float* cos_sin;  // [num_positions, rot]: cosines, then sines
+  const int32_t* positions;
+  const int64_t* slots;
+  void* q_out;
+  void* k_out;
+  void* v_out;  // nullptr: v goes to the pool only
+  void* k_pool;
+  void* v_pool;
+  const float* k_scale;
+  const float* v_scale;
+  int64_t q_stride, k_stride, v_stride;  // elements from one token's heads to the next's
+  float eps;
+  int32_t num_tokens;
+  int32_t hq, hkv;
+  int32_t num_positions;
+  int32_t rot;
+  int32_t num_pages;
+  int32_t page_size;
+  int32_t splits;  // waves per token
 };
 
 // Sets the thread-local message returned by cw_last_error_message.
@@ -189,6 +249,17 @@ hipError_t launch_stage_copy(const void* src, void* dst, size_t bytes, hipStream
 // multiple of 4; for calls captured into a graph).
 constexpr size_t kArgChunkBytes = 2048;
 hipError_t launch_arg_copy(const void* src, void* dst, size_t bytes, hipStream_t stream);
+hipError_t launch_diff_extend(const DiffParams& p, int head_dim, int page_size, bool fp8, hipStream_t stream,
+                              const ArgPlanBuf* ap = nullptr);
+hipError_t launch_diff_decode(const DiffParams& p, int head_dim, int page_size, bool fp8, hipStream_t stream,
+                              const ArgPlanBuf* ap = nullptr);
+int diff_decode_keys_per_tile();
+int diff_decode_waves_per_cu(int head_dim, bool fp8);
+hipError_t launch_diff_combine(const DiffParams& p, int head_dim, int max_parts, hipStream_t stream,
+                               const ArgPlanBuf* ap = nullptr);
+hipError_t launch_step_tables(const StepTablesParams& p, hipStream_t stream);
+// pool: 0 no page write, 1 bf16 pools, 2 fp8 pools
+hipError_t launch_qk_norm_rope(NormRopeParams p, int head_dim, bool interleaved, int pool, hipStream_t stream);
 hipError_t launch_check_table(const int32_t* bt, int32_t bt_stride, int32_t num_pages,
                               const SeqInfo* seqs, int32_t num_seqs, int32_t page_size,
                               int32_t* bad, hipStream_t stream);

@@ -1,0 +1,433 @@
+// Differential attention of single new tokens over a paged cache, HBM-streaming.
+//
+// Work item = one wave: the G <= 16 query pairs of one key pair against a chunk of at most
+// 64 pages of one sequence's prefix, plus the new token's own key when the chunk ends the
+// sequence.  Every cached K/V byte is read once, so the kernel is bound by HBM.
+//
+// Both maps share one accumulator: columns 0-15 of the 32 of an MFMA are the first map's
+// queries, columns 16-31 the second's.  S^T = K1 [Q1 | 0] + K2 [0 | Q2] (the zeros cost
+// matrix cycles, which a streaming kernel has to spare), one softmax pass serves both
+// maps, and O^T += V^T P^T multiplies both maps' weights with a value row read once.
+//
+// A tile is 32 keys: rows of both key heads and both value halves, DMA'd into LDS by
+// global_load_lds_dwordx4 with the kernel's own vmcnt waits (see the decode kernel, whose
+// pipeline this is).  Bytes in flight per CU decide: 32 KB tiles (D = 128, bf16) in two
+// stages and two waves per CU, smaller ones in three stages and three or six waves:
+// 128-144 KB of LDS.  fp8 pools keep their codes in LDS and are widened exactly to bf16;
+// a page's K scale of each map multiplies that map's scores, the V scales of the two
+// halves multiply the weights (one set of weights per half).
+#include <hip/hip_runtime.h>
+
+#include "../cw_internal.h"
+#include "../plan_expand.h"
+#include "diff_common.h"
+
+namespace cw {
+namespace {
+
+using namespace diff;
+
+constexpr int kScalarSearchSeqs = 8;  // up to here an item's sequence is searched by scalar loads
+constexpr int kKeys = 32;             // keys of a tile
+
+// 16 bytes per lane from global memory straight into LDS (lane l at LDS address m0 + 16 l),
+// nontemporal: every byte is read once.  Inline assembly, so that the compiler does not
+// drain the DMA in flight at the loop header; the kernel's own waits order it.
+__device__ __forceinline__ void dma16(const void* src, uint32_t lds_addr) {
+  asm volatile("global_load_lds_dwordx4 %0, off nt" ::"v"(src), "{m0}"(lds_addr) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void wait_vmcnt() {
+  static_assert(N >= 0 && N < 64, "vmcnt range");
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void wait_lgkmcnt0() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ uint32_t lds_addr(const void* p) {
+  return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((const lds_void*)p));
+}
+
+template <bool HI>
+__device__ __forceinline__ uint32_t fp8x2_bf16x2(uint32_t v) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(static_cast<int>(v), 1.0f, HI));
+}
+__device__ __forceinline__ bf16x8 fp8x8_bf16x8(u32x2 c) {
+  const u32x4 r = {fp8x2_bf16x2<false>(c.x), fp8x2_bf16x2<true>(c.x), fp8x2_bf16x2<false>(c.y), fp8x2_bf16x2<true>(c.y)};
+  return __builtin_bit_cast(bf16x8, r);
+}
+
+__host__ __device__ constexpr int tile_bytes(int d, bool fp8) { return 4 * kKeys * d * (fp8 ? 1 : 2); }
+__host__ __device__ constexpr int stages(int d, bool fp8) { return tile_bytes(d, fp8) > 16384 ? 2 : 3; }
+
+template <int D, int P, bool FP8>
+struct Geo {
+  static constexpr int RB = D * (FP8 ? 1 : 2);      // bytes per row
+  static constexpr int MAT = kKeys * RB;            // bytes of one matrix of a tile: K1, K2, Va, Vb
+  static constexpr int TILE = 4 * MAT;
+  static constexpr int STAGES = stages(D, FP8);
+  static constexpr int CPR = RB / 16;               // 16-byte chunks per row
+  static constexpr int RPI = 64 / CPR;              // rows per DMA instruction
+  static constexpr int NI = kKeys / RPI;            // DMA instructions per matrix
+  static constexpr int DMA = 4 * NI;                // per tile
+  static constexpr int KT = D / 16;                 // k-steps of K Q^T
+  static constexpr int DB = D / 32;                 // 32-row blocks of O^T per value half
+  static constexpr int VB = 2 * DB;
+  static_assert(RPI <= 16, "an instruction's rows lie in one page");
+  static_assert((STAGES - 1) * DMA < 64, "vmcnt range");
+};
+
+// Chunk swizzles for conflict-free LDS reads, as in the decode kernel
+template <int RB>
+__device__ __forceinline__ int k_swz(int row) {
+  const int s = swap_bits_2_3(row);
+  return RB == 256 ? (s & 15) : RB == 128 ? ((s >> 1) & 7) : ((s >> 2) & 3);
+}
+template <int RB>
+__device__ __forceinline__ int v_swz16(int row) {
+  return RB == 256 ? 4 * (row & 3) : 4 * ((row >> 1) & 1);
+}
+template <int RB>
+__device__ __forceinline__ int v_swz8(int row) {
+  return RB == 128 ? 2 * ((row >> 1) & 3) : 2 * ((row >> 2) & 1);
+}
+
+template <int D, int P, bool FP8, int AP>
+__global__ __launch_bounds__(64) void diff_decode_kernel(DiffParams dp, PlanArg<AP> ap) {
+  using T = Geo<D, P, FP8>;
+  const ExtendParams& p = dp.a;
+  // one array per stage: every step addresses a fixed array
+  __shared__ __attribute__((aligned(1024))) uint8_t lds_s0[T::TILE];
+  __shared__ __attribute__((aligned(1024))) uint8_t lds_s1[T::TILE];
+  __shared__ __attribute__((aligned(1024))) uint8_t lds_s2[T::STAGES > 2 ? T::TILE : 16];
+
+  WorkItem it;
+  if constexpr (AP != kPlanInMemory) {  // the plan in the kernel arguments, in compact form
+    const ExpandDesc& d = *reinterpret_cast<const ExpandDesc*>(ap.bytes + p.ap_desc);
+    const DecodeRec* rec = reinterpret_cast<const DecodeRec*>(ap.bytes + d.rec_off);
+    const int i = blockIdx.x;
+    int b_full = 0;
+    if (i < d.n_full) {
+      if (d.n_seqs <= kScalarSearchSeqs) {
+        for (int k = 1; k < d.n_seqs; ++k) b_full += rec[k].full_off <= i ? 1 : 0;  // scalar loads
+      } else {
+        b_full = wave_last_at_most(d.n_seqs, i, static_cast<int>(threadIdx.x), [&](int k) { return rec[k].full_off; });
+      }
+    }
+    it = expand_item_at(rec, reinterpret_cast<const int32_t*>(ap.bytes + d.tail_off), d, i, b_full);
+  } else {
+    it = p.items[blockIdx.x];
+  }
+  if (it.seq < 0) return;
+  const SeqInfo sq = plan_ptr<AP>(ap, p.ap_seqs, p.seqs)[it.seq];
+  const int lane = threadIdx.x;
+  const int h = lane >> 5, col = lane & 31;
+  const int map = col >> 4, g = col & 15;  // this lane's column: a map and a query pair
+  const int G = p.gqa_group, hkv = 2 * p.num_kv_heads, hp = p.num_kv_heads * G;
+  const int pair = it.kvh;
+  const int lp = sq.lp;
+  const int tok = sq.cu;  // the sequence's single new token
+  const int32_t* bt = p.block_table + size_t(sq.bt_row) * p.bt_stride;
+  const uint8_t* k_pool = static_cast<const uint8_t*>(p.k_pool);
+  const uint8_t* v_pool = static_cast<const uint8_t*>(p.v_pool);
+  const bool row_ok = g < G;
+
+  // prefix keys of this item: [kb, ke); the new key when kv_end passes lp
+  const int kb = it.kv_begin;
+  const int ke = min(it.kv_end, lp);
+  const bool has_new = it.kv_end > lp;
+  const int n_tiles = ke > kb ? (ke - kb + kKeys - 1) / kKeys : 0;
+
+  // page ids (and fp8 scales) of the chunk: lane j holds page kb / P + j
+  const int page0 = kb / P;
+  const int n_pages = ke > kb ? (ke - 1) / P - page0 + 1 : 0;
+  int my_pg = 0;
+  float my_ks[2] = {1.f, 1.f}, my_vs[2] = {1.f, 1.f};
+  if (lane < n_pages) {
+    my_pg = bt[page0 + lane];
+    if constexpr (FP8) {
+      const size_t si = size_t(my_pg) * hkv + 2 * pair;
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        my_ks[m] = p.k_scale[si + m];
+        my_vs[m] = p.v_scale[si + m];
+      }
+    }
+  }
+
+  // Q^T (B operand): this column's query, the other map's operand zero.  bf16 pools: k-step
+  // kk holds dims 16 kk + 8 h + e; fp8 pools read 16 dims per fragment, so k-steps 2 t and 2
+  // t + 1 hold dims 32 t + 16 h + 8 (kk & 1) + e.  And the new token's key and value, used
+  // after the last tile, read here so that their latency does not end the item.
+  auto dim0 = [&](int kk) { return FP8 ? 32 * (kk >> 1) + 16 * h + 8 * (kk & 1) : 16 * kk + 8 * h; };
+  bf16x8 qf[2][T::KT];
+  {
+    const uint16_t* qrow =
+        static_cast<const uint16_t*>(p.q) + (2 * (size_t(tok) * hp + size_t(pair) * G + g) + map) * D;
+#pragma unroll
+    for (int kk = 0; kk < T::KT; ++kk) {
+      u32x4 v = {0u, 0u, 0u, 0u};
+      const u32x4 zero = v;
+      if (row_ok) v = *reinterpret_cast<const u32x4*>(qrow + dim0(kk));
+      qf[0][kk] = __builtin_bit_cast(bf16x8, map == 0 ? v : zero);
+      qf[1][kk] = __builtin_bit_cast(bf16x8, map == 0 ? zero : v);
+    }
+  }
+  bf16x8 k_own[T::KT];
+  bf16x4 v_own[T::VB][4];
+  if (has_new) {
+    const uint16_t* kn = static_cast<const uint16_t*>(p.k_new) + (size_t(tok) * hkv + 2 * pair + map) * D;
+    const uint16_t* vn = static_cast<const uint16_t*>(p.v_new) + (size_t(tok) * hkv + 2 * pair) * D;  // both halves
+#pragma unroll
+    for (int kk = 0; kk < T::KT; ++kk) k_own[kk] = *reinterpret_cast<const bf16x8*>(kn + dim0(kk));
+#pragma unroll
+    for (int b = 0; b < T::VB; ++b)
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4) v_own[b][q4] = *reinterpret_cast<const bf16x4*>(vn + 32 * b + 8 * q4 + 4 * h);
+  }
+
+  // DMA of tile t: instruction j of a matrix covers tile rows [j RPI, (j + 1) RPI); rows past
+  // the chunk's prefix end fetch its last key again (their scores are masked), so every tile
+  // issues exactly DMA instructions and the wait counts below are exact.
+  const int dma_row = lane / T::CPR, dma_pos = lane % T::CPR;
+  auto issue_tile = [&](int t, uint32_t dst) __attribute__((always_inline)) {
+    const int j0 = kb + t * kKeys;
+#pragma unroll
+    for (int j = 0; j < T::NI; ++j) {
+      const int R = j * T::RPI + dma_row;
+      const int key = min(j0 + R, ke - 1);
+      const int r0 = min(j0 + j * T::RPI, ke - 1);  // (uniform)
+      const int pg = __builtin_amdgcn_readlane(my_pg, min(r0 / P - page0, 63));
+      const size_t base = (size_t(pg) * hkv + 2 * pair) * P * T::RB + size_t(key % P) * T::RB;
+      const uint32_t kc = 16 * (dma_pos ^ k_swz<T::RB>(R));
+      const uint32_t vc = 16 * (dma_pos ^ (FP8 ? v_swz8<T::RB>(R) : v_swz16<T::RB>(R)));
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        dma16(k_pool + base + m * (P * T::RB) + kc, dst + m * T::MAT + j * T::RPI * T::RB);
+        dma16(v_pool + base + m * (P * T::RB) + vc, dst + (2 + m) * T::MAT + j * T::RPI * T::RB);
+      }
+    }
+  };
+
+  f32x16 o[T::VB];
+#pragma unroll
+  for (int b = 0; b < T::VB; ++b) o[b] = f32x16{};
+  float m_run = kNegBig, l_run = 0.f;
+  const float c = p.scale_log2;
+
+  // Q, the new token's rows and the page ids land first (the addresses need the ids), so
+  // only DMA is outstanding in the loop
+  __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8));
+  if (n_tiles > 0) issue_tile(0, lds_addr(lds_s0));
+  if (n_tiles > 1) issue_tile(1, lds_addr(lds_s1));
+  if (T::STAGES > 2 && n_tiles > 2) issue_tile(2, lds_addr(lds_s2));
+
+  auto compute = [&](int t, const uint8_t* st) __attribute__((always_inline)) {
+    const int j0 = kb + t * kKeys;
+    f32x16 s = f32x16{};
+    const int R = swap_bits_2_3(col);  // row m of the block reads key swap(m)
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      const uint8_t* km = st + m * T::MAT + R * T::RB;
+      if constexpr (FP8) {
+#pragma unroll
+        for (int t2 = 0; t2 < T::KT / 2; ++t2) {
+          const u32x4 raw = *reinterpret_cast<const u32x4*>(km + 16 * ((2 * t2 + h) ^ k_swz<T::RB>(R)));
+          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fp8x8_bf16x8(u32x2{raw.x, raw.y}), qf[m][2 * t2], s, 0, 0, 0);
+          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fp8x8_bf16x8(u32x2{raw.z, raw.w}), qf[m][2 * t2 + 1], s, 0, 0, 0);
+        }
+      } else {
+#pragma unroll
+        for (int kk = 0; kk < T::KT; ++kk) {
+          const bf16x8 kf = *reinterpret_cast<const bf16x8*>(km + 16 * ((2 * kk + h) ^ k_swz<T::RB>(R)));
+          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[m][kk], s, 0, 0, 0);
+        }
+      }
+    }
+    // element i holds key j0 + 16 (i / 8) + 8 h + i % 8; the keys of half-group i / 8 share a page
+    float cg[2] = {c, c}, vs[2][2] = {{1.f, 1.f}, {1.f, 1.f}};
+    if constexpr (FP8) {
+#pragma unroll
+      for (int s8 = 0; s8 < 2; ++s8) {
+        const int q = min((j0 + 16 * s8) / P - page0, 63);
+        const float k0 = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(my_ks[0]), q));
+        const float k1 = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(my_ks[1]), q));
+        cg[s8] = c * (map == 0 ? k0 : k1);
+#pragma unroll
+        for (int m = 0; m < 2; ++m) vs[s8][m] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(my_vs[m]), q));
+      }
+    }
+    if (j0 + kKeys > ke) {  // keys past the chunk's prefix end
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (j0 + 16 * (i >> 3) + 8 * h + (i & 7) >= ke) s[i] = -INFINITY;
+    }
+    // weights against the running max as it stands; raised only when a half-column's sum
+    // passes kSumLimit (or is not finite, as on an item's first tile)
+    float w[16], tsum;
+    auto weights = [&]() __attribute__((always_inline)) {
+      tsum = 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        w[i] = __builtin_amdgcn_exp2f(fmaf(s[i], cg[i >> 3], -m_run));
+        tsum += w[i];
+      }
+    };
+    weights();
+    if (__any(!(tsum <= kSumLimit))) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[i] * cg[i >> 3]);
+      mx = row_max(mx);
+      if (mx > m_run) {
+        const float alpha = __builtin_amdgcn_exp2f(m_run - mx);
+        m_run = mx;
+        l_run *= alpha;
+#pragma unroll
+        for (int b = 0; b < T::VB; ++b) o[b] *= alpha;
+      }
+      weights();
+    }
+    l_run += tsum;
+    // O^T += V^T P^T over the tile's two 16-key slices
+    const int grp = lane >> 4, ri = lane & 15;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const uint8_t* vt = st + (2 + half) * T::MAT;
+        bf16x8 pf;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) pf[e] = static_cast<__bf16>(FP8 ? w[8 * u + e] * vs[u][half] : w[8 * u + e]);
+#pragma unroll
+        for (int b = 0; b < T::DB; ++b) {
+          bf16x8 vf;
+          if constexpr (FP8) {
+            // source lane (k, a) = (ri / 2, ri % 2): key 16 u + 8 h + k, dims 32 b + 16 (grp & 1) + 8 a
+            const int Rv = 16 * u + 8 * h + (ri >> 1);
+            const int dbyte = 32 * b + 16 * (grp & 1) + 8 * (ri & 1);
+            const int off = Rv * T::RB + 16 * ((dbyte >> 4) ^ v_swz8<T::RB>(Rv)) + (dbyte & 15);
+            const i32x2 raw = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)(vt + off));
+            vf = fp8x8_bf16x8(u32x2{static_cast<uint32_t>(raw.x), static_cast<uint32_t>(raw.y)});
+          } else {
+            const int kq = ri >> 2, a = ri & 3;
+            const int chunk = 4 * b + 2 * (grp & 1) + (a >> 1);
+            i16x4 part[2];
+#pragma unroll
+            for (int e4 = 0; e4 < 2; ++e4) {
+              const int Rv = 16 * u + 8 * h + 4 * e4 + kq;
+              const int off = Rv * T::RB + 16 * (chunk ^ v_swz16<T::RB>(Rv)) + 8 * (a & 1);
+              part[e4] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(vt + off));
+            }
+            vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
+          }
+          o[half * T::DB + b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, o[half * T::DB + b], 0, 0, 0);
+        }
+      }
+    }
+  };
+  // Tile t lives in stage t % STAGES.  A step waits for its tile (those issued after it may
+  // still fly), computes on it, then refills the stage if there is a tile for it.
+  auto step = [&](int t, const uint8_t* st) __attribute__((always_inline)) {
+    const int behind = n_tiles - 1 - t;
+    if (T::STAGES > 2 && behind >= 2) wait_vmcnt<(T::STAGES - 1) * T::DMA>();
+    else if (behind >= 1) wait_vmcnt<T::DMA>();
+    else wait_vmcnt<0>();
+    compute(t, st);
+    if (behind >= T::STAGES) {
+      wait_lgkmcnt0();  // the stage's reads are done before it is refilled
+      issue_tile(t + T::STAGES, lds_addr(st));
+    }
+  };
+  for (int t = 0; t < n_tiles; t += T::STAGES) {
+    step(t, lds_s0);
+    if (t + 1 < n_tiles) step(t + 1, lds_s1);
+    if constexpr (T::STAGES > 2) {
+      if (t + 2 < n_tiles) step(t + 2, lds_s2);
+    }
+  }
+  wait_vmcnt<0>();  // no DMA may land in LDS after the wave has ended
+
+  if (has_new) {  // the new token's own key and value (bf16)
+    float part = 0.f;
+#pragma unroll
+    for (int kk = 0; kk < T::KT; ++kk) {
+      const bf16x8 q = map == 0 ? qf[0][kk] : qf[1][kk];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) part = fmaf(static_cast<float>(q[e]), static_cast<float>(k_own[kk][e]), part);
+    }
+    const float x = row_sum(part) * c;
+    const float m_new = fmaxf(m_run, x);
+    const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+    const float pn = __builtin_amdgcn_exp2f(x - m_new);
+    m_run = m_new;
+    l_run = l_run * alpha + (h == 0 ? pn : 0.f);
+#pragma unroll
+    for (int b = 0; b < T::VB; ++b)
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          o[b][4 * q4 + e] = fmaf(pn, static_cast<float>(v_own[b][q4][e]), o[b][4 * q4 + e] * alpha);
+  }
+
+  const float l_tot = row_sum(l_run);
+  if (it.part >= 0) {  // unnormalised partials of both maps, merged by diff_combine
+    if (!row_ok) return;
+    const size_t slot = size_t(it.part) * p.part_rows + map * (p.part_rows / 2) + g;
+    float* po = static_cast<float*>(p.part_o) + slot * (2 * D);
+#pragma unroll
+    for (int b = 0; b < T::VB; ++b)
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4)
+        *reinterpret_cast<f32x4*>(po + 32 * b + 8 * q4 + 4 * h) =
+            f32x4{o[b][4 * q4], o[b][4 * q4 + 1], o[b][4 * q4 + 2], o[b][4 * q4 + 3]};
+    if (h == 0) *reinterpret_cast<f32x2*>(p.part_ml + slot * 2) = f32x2{m_run, l_tot};
+    return;
+  }
+  // the second map's columns give lam O2 / l2 to the first map's (lanes l and l + 16)
+  const float f = (map == 0 ? 1.f : row_ok ? dp.lam[pair * G + g] : 0.f) / l_tot;
+#pragma unroll
+  for (int b = 0; b < T::VB; ++b)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float mine = o[b][i] * f;
+      o[b][i] = mine - __shfl_xor(mine, 16);
+    }
+  if (map == 0 && row_ok)
+    store_row<T::VB>(dp, static_cast<uint16_t*>(p.out) + (size_t(tok) * hp + size_t(pair) * G + g) * (2 * D), h, o);
+}
+
+template <int D, int P, bool FP8>
+hipError_t launch_t(const DiffParams& p, hipStream_t stream, const ArgPlanBuf* ap) {
+  const dim3 grid(p.a.n_items), block(64);
+  if (ap != nullptr && ap->small())
+    hipLaunchKernelGGL((diff_decode_kernel<D, P, FP8, kPlanInSmallArgs>), grid, block, 0, stream, p, ap->small_plan());
+  else if (ap != nullptr)
+    hipLaunchKernelGGL((diff_decode_kernel<D, P, FP8, kPlanInArgs>), grid, block, 0, stream, p, ap->plan);
+  else
+    hipLaunchKernelGGL((diff_decode_kernel<D, P, FP8, kPlanInMemory>), grid, block, 0, stream, p, NoArgPlan{});
+  return hipGetLastError();
+}
+
+}  // namespace
+
+int diff_decode_keys_per_tile() { return kKeys; }
+
+int diff_decode_waves_per_cu(int head_dim, bool fp8) {  // 160 KB of LDS per CU
+  return (160 * 1024) / (stages(head_dim, fp8) * tile_bytes(head_dim, fp8));
+}
+
+hipError_t launch_diff_decode(const DiffParams& p, int head_dim, int page_size, bool fp8, hipStream_t stream,
+                              const ArgPlanBuf* ap) {
+  if (p.a.n_items <= 0) return hipSuccess;
+#define CW_CASE(D_, P_)                  \
+  if (head_dim == D_ && page_size == P_) \
+    return fp8 ? launch_t<D_, P_, true>(p, stream, ap) : launch_t<D_, P_, false>(p, stream, ap);
+  CW_CASE(64, 16)
+  CW_CASE(64, 64)
+  CW_CASE(128, 16)
+  CW_CASE(128, 64)
+#undef CW_CASE
+  return hipErrorInvalidValue;
+}
+
+}  // namespace cw

@@ -416,9 +416,10 @@ ExtendPlan build_extend_plan(const int32_t* prefix_lens, const int32_t* suffix_l
                              int32_t num_seqs, int32_t num_kv_heads, int32_t gqa_group,
                              int32_t head_dim, int32_t block_m, int32_t wgs_per_cu,
                              int32_t num_cus, int32_t num_xcds, const Tuning& tuning,
-                             const int32_t* cu_rows, const int32_t* bt_rows) {
+                             const int32_t* cu_rows, const int32_t* bt_rows, int32_t maps) {
   ExtendPlan plan;
-  plan.part_rows = block_m;
+  plan.part_rows = block_m * maps;
+  plan.part_f32 = maps > 1;
   plan.seqs.resize(num_seqs);
   int64_t cu = 0, n_tiles = 0;
   for (int32_t b = 0; b < num_seqs; ++b) {
@@ -703,9 +704,9 @@ ExtendPlan build_decode_plan(const int32_t* prefix_lens, int32_t num_seqs, int32
                              int32_t gqa_group, int32_t head_dim, int32_t page_size,
                              int32_t keys_per_tile, int32_t waves_per_cu, int32_t num_cus,
                              const Tuning& tuning, size_t meta_at, const int32_t* cu_rows,
-                             const int32_t* bt_rows) {
+                             const int32_t* bt_rows, int32_t maps) {
   ExtendPlan plan;
-  plan.part_rows = gqa_group;
+  plan.part_rows = gqa_group * maps;
   plan.seqs.resize(num_seqs);
   int64_t total_tiles = 0;
   for (int32_t b = 0; b < num_seqs; ++b) {
@@ -770,7 +771,7 @@ ExtendPlan build_decode_plan(const int32_t* prefix_lens, int32_t num_seqs, int32
     return (a.kv_end - a.kv_begin) > (c.kv_end - c.kv_begin);
   });
   plan.items.insert(plan.items.end(), tails.begin(), tails.end());
-  plan.part_f32 = chunk != plain_chunk;
+  plan.part_f32 = maps > 1 || chunk != plain_chunk;
   layout_workspace(plan, head_dim);
   plan.whole_meta_bytes = plan.meta_bytes;
   if (chunk != plain_chunk) {

@@ -61,12 +61,15 @@ struct ExtendPlan {
 // which `wgs_per_cu` are resident per CU.  `num_cus` and `num_xcds` describe
 // the device.  Lengths must already be validated.  Sequence b's first packed
 // row is cu_rows[b] and its block-table row bt_rows[b] when given (a sub-batch
-// of a larger step), else the prefix sum of the suffix lengths and b.
+// of a larger step), else the prefix sum of the suffix lengths and b.  With `maps` softmax
+// maps per query row a partial slot has maps * block_m rows of head_dim values, fp32 when
+// there are more than one (what the merge subtracts is not rounded before).
 ExtendPlan build_extend_plan(const int32_t* prefix_lens, const int32_t* suffix_lens,
                              int32_t num_seqs, int32_t num_kv_heads, int32_t gqa_group,
                              int32_t head_dim, int32_t block_m, int32_t wgs_per_cu,
                              int32_t num_cus, int32_t num_xcds, const Tuning& tuning,
-                             const int32_t* cu_rows = nullptr, const int32_t* bt_rows = nullptr);
+                             const int32_t* cu_rows = nullptr, const int32_t* bt_rows = nullptr,
+                             int32_t maps = 1);
 
 // Bytes of a decode plan in compact form whose records start at byte `at`.
 inline size_t compact_bytes(size_t at, size_t n_seqs, size_t n_tails) {
@@ -77,12 +80,12 @@ inline bool compact_arg_fits(size_t bytes) { return bytes + sizeof(ExpandDesc) <
 
 // Decode plan (every suffix length 1): one item per (sequence, kv head, key
 // chunk) with `gqa_group` rows; `keys_per_tile` is the decode kernel's tile.  The
-// plan's meta starts at byte `meta_at` of its call's.
+// plan's meta starts at byte `meta_at` of its call's.  `maps` as above.
 ExtendPlan build_decode_plan(const int32_t* prefix_lens, int32_t num_seqs, int32_t num_kv_heads,
                              int32_t gqa_group, int32_t head_dim, int32_t page_size,
                              int32_t keys_per_tile, int32_t waves_per_cu, int32_t num_cus,
                              const Tuning& tuning, size_t meta_at = 0, const int32_t* cu_rows = nullptr,
-                             const int32_t* bt_rows = nullptr);
+                             const int32_t* bt_rows = nullptr, int32_t maps = 1);
 
 // Serialises seqs, items and groups into `dst` (meta_bytes long) at their offsets.
 void pack_plan_meta(const ExtendPlan& plan, uint8_t* dst);
