@@ -245,14 +245,15 @@ void diff_extend_kernel(DiffParams dp, PlanArg<AP> ap) {
   const uint8_t* k_pool_pair = k_pool + size_t(2 * pair) * page_bytes;
   const uint8_t* v_pool_pair = v_pool + size_t(2 * pair) * page_bytes;
   const size_t page_stride = size_t(hkv) * page_bytes;
-  // fp8 pool rows of both matrices into registers, with their page's scales
+  // fp8 pool rows of both matrices into registers, with their page's scales (`in_prefix`: the
+  // tile lies wholly in the cached prefix, so every row check passes)
   struct Rows8 {
     u32x4 x[2];
     float s[2];
   };
   auto load8 = [&](int j0, int pg, const uint8_t* pool_pair, const_f32* scales, const uint32_t(&off)[2],
-                   Rows8& rw) __attribute__((always_inline)) {
-    if (j0 + wrow0 >= lp) return;
+                   Rows8& rw, bool in_prefix) __attribute__((always_inline)) {
+    if (!in_prefix && j0 + wrow0 >= lp) return;
     const auto rs = rsrc_at(pool_pair + size_t(pg) * page_stride);
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
@@ -266,18 +267,18 @@ void diff_extend_kernel(DiffParams dp, PlanArg<AP> ap) {
       }
     }
   };
-  auto store8 = [&](int j0, int from, const Rows8& rw, uint8_t* dst, bool is_k) __attribute__((always_inline)) {
-    if (j0 + wrow0 >= lp || j0 + wrow0 + 7 < from) return;
+  auto store8 = [&](int j0, int from, const Rows8& rw, uint8_t* dst, bool in_prefix) __attribute__((always_inline)) {
+    if (!in_prefix && (j0 + wrow0 >= lp || j0 + wrow0 + 7 < from)) return;
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
       const PageScale sc = page_scale(rw.s[m]);
       if constexpr (T::B8 == 16) {
-        if (j0 + r8[0] < lp)
+        if (in_prefix || j0 + r8[0] < lp)
           *reinterpret_cast<u32x4*>(dst + m * T::TILE + wrow0 * T::RB + 16 * lane) = fp8x8_f16x8(rw.x[m].x, rw.x[m].y, sc);
-        if (j0 + r8[1] < lp)
+        if (in_prefix || j0 + r8[1] < lp)
           *reinterpret_cast<u32x4*>(dst + m * T::TILE + (wrow0 + 4) * T::RB + 16 * lane) =
               fp8x8_f16x8(rw.x[m].z, rw.x[m].w, sc);
-      } else if (j0 + r8[0] < lp) {
+      } else if (in_prefix || j0 + r8[0] < lp) {
         *reinterpret_cast<u32x4*>(dst + m * T::TILE + wrow0 * T::RB + 16 * lane) = fp8x8_f16x8(rw.x[m].x, rw.x[m].y, sc);
       }
     }
@@ -433,16 +434,16 @@ void diff_extend_kernel(DiffParams dp, PlanArg<AP> ap) {
     pg_v = load_page(tile0(1));
     if constexpr (FP8) {
       Rows8 kp{}, kf{}, vf{};
-      if (wrow0 >= kAhead) load8(b0 - kAhead, pgp, k_pool_pair, ks_s, k8_off, kp);
-      load8(b0 + kAhead, pk0, k_pool_pair, ks_s, k8_off, kf);
-      load8(b0, pv0, v_pool_pair, vs_s, v8_off, vf);
+      if (wrow0 >= kAhead) load8(b0 - kAhead, pgp, k_pool_pair, ks_s, k8_off, kp, false);
+      load8(b0 + kAhead, pk0, k_pool_pair, ks_s, k8_off, kf, false);
+      load8(b0, pv0, v_pool_pair, vs_s, v8_off, vf, false);
       __builtin_amdgcn_s_waitcnt(0);
-      if (wrow0 >= kAhead) store8(b0 - kAhead, b0, kp, lds_k1, true);
-      store8(b0 + kAhead, 0, kf, lds_k0, true);
+      if (wrow0 >= kAhead) store8(b0 - kAhead, b0, kp, lds_k1, false);
+      store8(b0 + kAhead, 0, kf, lds_k0, false);
       store8(b0, 0, vf, lds_v0, false);
       convert_new(b0 - kAhead, b0, lds_k1);
-      load8(tile0(1) + kAhead, pg_k, k_pool_pair, ks_s, k8_off, k8);
-      load8(tile0(1), pg_v, v_pool_pair, vs_s, v8_off, v8);
+      load8(tile0(1) + kAhead, pg_k, k_pool_pair, ks_s, k8_off, k8, false);
+      load8(tile0(1), pg_v, v_pool_pair, vs_s, v8_off, v8, false);
       pg_k = load_page(tile0(2) + kAhead);
       pg_v = load_page(tile0(2));
     }
@@ -458,24 +459,24 @@ void diff_extend_kernel(DiffParams dp, PlanArg<AP> ap) {
 
   // iteration j: key tile j (scores of the blocks after this tile's first) and value tile
   // j are resident; tiles j + 1 go to the other stages
-  auto iteration = [&](int j, const uint8_t* k_cur, uint8_t* k_nxt, const uint8_t* v_cur, uint8_t* v_nxt,
-                       uint8_t* k_mine, uint8_t* v_mine) __attribute__((always_inline)) {
+  auto iteration = [&](int j, uint8_t* k_cur, uint8_t* k_nxt, uint8_t* v_cur,
+                       uint8_t* v_nxt) __attribute__((always_inline)) {
     __builtin_amdgcn_s_waitcnt(0);  // this wave's staging of tile j has landed
     if constexpr (FP8) {
-      convert_new(tile0(j) + kAhead, 0, k_mine);
-      convert_new(tile0(j), 0, v_mine);
+      convert_new(tile0(j) + kAhead, 0, k_cur);
+      convert_new(tile0(j), 0, v_cur);
     }
     __syncthreads();  // everyone's has; the other stages are no longer read
     if (j + 1 < n_tiles) {
       if constexpr (FP8) {
-        store8(tile0(j + 1) + kAhead, 0, k8, k_nxt, true);
+        store8(tile0(j + 1) + kAhead, 0, k8, k_nxt, false);
         store8(tile0(j + 1), 0, v8, v_nxt, false);
       }
       issue(tile0(j + 1) + kAhead, 0, k_nxt, pg_k, k_pool, k_new, k_off, kn_off);
       issue(tile0(j + 1), 0, v_nxt, pg_v, v_pool, v_new, v_off, vn_off);
       if constexpr (FP8) {
-        load8(tile0(j + 2) + kAhead, pg_k, k_pool_pair, ks_s, k8_off, k8);
-        load8(tile0(j + 2), pg_v, v_pool_pair, vs_s, v8_off, v8);
+        load8(tile0(j + 2) + kAhead, pg_k, k_pool_pair, ks_s, k8_off, k8, false);
+        load8(tile0(j + 2), pg_v, v_pool_pair, vs_s, v8_off, v8, false);
       }
       pg_k = load_page(tile0(j + (FP8 ? 3 : 2)) + kAhead);
       pg_v = load_page(tile0(j + (FP8 ? 3 : 2)));
@@ -484,9 +485,90 @@ void diff_extend_kernel(DiffParams dp, PlanArg<AP> ap) {
     step(k_cur, v_cur, 0, tile0(j) + 32, true, xa, xb);
     step(k_cur, v_cur, 1, tile0(j) + 64, true, xb, xa);
   };
-  for (int j = 0; j < n_tiles; j += 2) {
-    iteration(j, lds_k0, lds_k1, lds_v0, lds_v1, lds_k0, lds_v0);
-    if (j + 1 < n_tiles) iteration(j + 1, lds_k1, lds_k0, lds_v1, lds_v0, lds_k1, lds_v1);
+  // Iterations whose staged tiles lie wholly in the cached prefix (fp8: whose loaded tiles do
+  // too): every row sees all their keys and a wave's rows come from one page, so they carry
+  // no mode decisions and no mask.
+  auto issue_prefix = [&](uint8_t* dst, int pg, const uint8_t* pool_pair,
+                          const uint32_t(&off)[T::NI]) __attribute__((always_inline)) {
+    const auto rs = rsrc_at(pool_pair + size_t(pg) * page_stride);
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int i = 0; i < T::NI; ++i)
+        dma16(rs, (lds_void*)(dst + m * T::TILE + (wrow0 + T::RPI * i) * T::RB), off[i], m * page_bytes);
+  };
+  auto steady = [&](int j, const uint8_t* k_cur, uint8_t* k_nxt, const uint8_t* v_cur,
+                    uint8_t* v_nxt) __attribute__((always_inline)) {
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    if constexpr (FP8) {
+      store8(tile0(j + 1) + kAhead, 0, k8, k_nxt, true);
+      store8(tile0(j + 1), 0, v8, v_nxt, true);
+      load8(tile0(j + 2) + kAhead, pg_k, k_pool_pair, ks_s, k8_off, k8, true);
+      load8(tile0(j + 2), pg_v, v_pool_pair, vs_s, v8_off, v8, true);
+    } else {
+      issue_prefix(k_nxt, pg_k, k_pool_pair, k_off);
+      issue_prefix(v_nxt, pg_v, v_pool_pair, v_off);
+    }
+    pg_k = load_page(tile0(j + (FP8 ? 3 : 2)) + kAhead);
+    pg_v = load_page(tile0(j + (FP8 ? 3 : 2)));
+    if (!wave_active) return;
+    step(k_cur, v_cur, 0, 0, false, xa, xb);
+    step(k_cur, v_cur, 1, 0, false, xb, xa);
+  };
+  // Iterations whose staged tiles lie wholly among the new tokens and whose scores every
+  // row of the workgroup sees.
+  auto issue_new = [&](int j0, uint8_t* dst, const uint8_t* fresh,
+                       const uint32_t(&noff)[T::NI]) __attribute__((always_inline)) {
+    const ptrdiff_t row0 = ptrdiff_t(sq.cu) + j0 - lp;
+    const auto rs = rsrc_at(fresh + (row0 * hkv + 2 * pair) * T::RB);
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int i = 0; i < T::NI; ++i)
+        dma16(rs, (lds_void*)(dst + m * T::TILE + (wrow0 + T::RPI * i) * T::RB), noff[i], m * T::RB);
+  };
+  auto steady_new = [&](int j, uint8_t* k_cur, uint8_t* k_nxt, uint8_t* v_cur,
+                        uint8_t* v_nxt) __attribute__((always_inline)) {
+    __builtin_amdgcn_s_waitcnt(0);
+    if constexpr (FP8) {
+      convert_new(tile0(j) + kAhead, 0, k_cur);
+      convert_new(tile0(j), 0, v_cur);
+    }
+    __syncthreads();
+    issue_new(tile0(j + 1) + kAhead, k_nxt, k_new, kn_off);
+    issue_new(tile0(j + 1), v_nxt, v_new, vn_off);
+    if (!wave_active) return;
+    step(k_cur, v_cur, 0, 0, false, xa, xb);
+    step(k_cur, v_cur, 1, 0, false, xb, xa);
+  };
+  // (floors: the numerators may be negative)
+  const int n_steady = min((lp - it.kv_begin - 96) >> 6, n_tiles - 1) - (FP8 ? 1 : 0);
+  const int new_begin = max(0, ((lp - it.kv_begin + 63) >> 6) - 1);
+  const int first_lim = lp + it.q_row0 / G + 1;
+  const int new_end = min(min((total_len - it.kv_begin - 96) >> 6, ((first_lim - it.kv_begin - 96) >> 6) + 1), n_tiles - 1);
+  int j = 0;
+  for (; j + 1 < n_steady; j += 2) {
+    steady(j, lds_k0, lds_k1, lds_v0, lds_v1);
+    steady(j + 1, lds_k1, lds_k0, lds_v1, lds_v0);
+  }
+  // (every loop takes two iterations at a time, so that an iteration's stages are fixed)
+  const int from = max(j, (new_begin + 1) & ~1);
+#pragma unroll 1
+  for (int rest = from + 1 < new_end ? 0 : 1; rest < 2; ++rest) {
+    const int to = rest == 0 ? from : n_tiles;
+#pragma unroll 1
+    for (; j < to; j += 2) {
+      iteration(j, lds_k0, lds_k1, lds_v0, lds_v1);
+      if (j + 1 < n_tiles) iteration(j + 1, lds_k1, lds_k0, lds_v1, lds_v0);
+    }
+    if (rest == 0) {
+#pragma unroll 1
+      for (; j + 1 < new_end; j += 2) {
+        steady_new(j, lds_k0, lds_k1, lds_v0, lds_v1);
+        steady_new(j + 1, lds_k1, lds_k0, lds_v1, lds_v0);
+      }
+    }
   }
 
   const float l_tot = row_sum(l_run);
