@@ -40,6 +40,11 @@ constexpr float kSumLimit = 65536.f;
 
 __device__ __forceinline__ int swap_bits_2_3(int r) { return (r & ~12) | ((r & 4) << 1) | ((r & 8) >> 1); }
 
+// The running max is set this much (in log2 units) below a row's largest score, so that fp16
+// weights down to 2^-22 of the largest are normal numbers (where a few keys take most of
+// the weight and many share the rest).
+constexpr float kHeadroom = 8.f;
+
 // Sum / maximum of a value over the two lanes (l and l + 32) that hold a row.
 __device__ __forceinline__ float row_sum(float x) {
   const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);

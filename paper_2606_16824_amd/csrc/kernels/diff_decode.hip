@@ -13,9 +13,9 @@
 // global_load_lds_dwordx4 with the kernel's own vmcnt waits (see the decode kernel, whose
 // pipeline this is).  Bytes in flight per CU decide: 32 KB tiles (D = 128, bf16) in two
 // stages and two waves per CU, smaller ones in three stages and three or six waves:
-// 128-144 KB of LDS.  fp8 pools keep their codes in LDS and are widened exactly to bf16;
-// a page's K scale of each map multiplies that map's scores, the V scales of the two
-// halves multiply the weights (one set of weights per half).
+// 128-144 KB of LDS.  fp8 pools keep their codes in LDS and are widened exactly (keys to
+// bf16, values to fp16); a page's K scale of each map multiplies that map's scores, the V
+// scales of the two halves multiply the weights (one set of weights per half).
 #include <hip/hip_runtime.h>
 
 #include "../cw_internal.h"
@@ -53,6 +53,16 @@ __device__ __forceinline__ uint32_t fp8x2_bf16x2(uint32_t v) {
 __device__ __forceinline__ bf16x8 fp8x8_bf16x8(u32x2 c) {
   const u32x4 r = {fp8x2_bf16x2<false>(c.x), fp8x2_bf16x2<true>(c.x), fp8x2_bf16x2<false>(c.y), fp8x2_bf16x2<true>(c.y)};
   return __builtin_bit_cast(bf16x8, r);
+}
+
+template <bool HI>
+__device__ __forceinline__ f16x2 fp8x2_f16x2(uint32_t v) {
+  return __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(static_cast<int>(v), 1.0f, HI);
+}
+__device__ __forceinline__ f16x8 fp8x8_f16x8(u32x2 c) {
+  const u32x4 r = {__builtin_bit_cast(uint32_t, fp8x2_f16x2<false>(c.x)), __builtin_bit_cast(uint32_t, fp8x2_f16x2<true>(c.x)),
+                   __builtin_bit_cast(uint32_t, fp8x2_f16x2<false>(c.y)), __builtin_bit_cast(uint32_t, fp8x2_f16x2<true>(c.y))};
+  return __builtin_bit_cast(f16x8, r);
 }
 
 __host__ __device__ constexpr int tile_bytes(int d, bool fp8) { return 4 * kKeys * d * (fp8 ? 1 : 2); }
@@ -150,6 +160,19 @@ __global__ __launch_bounds__(64) void diff_decode_kernel(DiffParams dp, PlanArg<
         my_ks[m] = p.k_scale[si + m];
         my_vs[m] = p.v_scale[si + m];
       }
+    }
+  }
+  // fp8: each half's largest V scale of the chunk is taken out of the weights (and multiplied
+  // back at the end), so that fp16 holds them whatever the scales' size
+  float vs_max[2] = {1.f, 1.f};
+  if constexpr (FP8) {
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      float x = lane < n_pages ? fabsf(my_vs[m]) : 0.f;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) x = fmaxf(x, __shfl_xor(x, d));
+      vs_max[m] = x > 0.f ? x : 1.f;
+      my_vs[m] /= vs_max[m];
     }
   }
 
@@ -272,11 +295,12 @@ __global__ __launch_bounds__(64) void diff_decode_kernel(DiffParams dp, PlanArg<
       }
     };
     weights();
-    if (__any(!(tsum <= kSumLimit))) {
+    // (half the limit: a single fp16 weight ends at 65504)
+    if (__any(!(tsum <= 0.5f * kSumLimit))) {
       float mx = -INFINITY;
 #pragma unroll
       for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[i] * cg[i >> 3]);
-      mx = row_max(mx);
+      mx = row_max(mx) - kHeadroom;
       if (mx > m_run) {
         const float alpha = __builtin_amdgcn_exp2f(m_run - mx);
         m_run = mx;
@@ -294,19 +318,32 @@ __global__ __launch_bounds__(64) void diff_decode_kernel(DiffParams dp, PlanArg<
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
         const uint8_t* vt = st + (2 + half) * T::MAT;
-        bf16x8 pf;
+        // Neither form of the weights adds to the output's own rounding.  bf16 pools: a weight
+        // is the sum of two bf16 (2^-16), for a second MFMA; fp8 pools: fp16 (2^-11), which
+        // holds the codes exactly too.  One bf16 weight each: relative error 2.4e-3 instead of
+        // 1.7e-3 at the same time (48 decodes: bf16 627 -> 634 us, fp8 351 -> 352 us).
+        bf16x8 pf, pl;
+        f16x8 ph;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) pf[e] = static_cast<__bf16>(FP8 ? w[8 * u + e] * vs[u][half] : w[8 * u + e]);
+        for (int e = 0; e < 8; ++e) {
+          if constexpr (FP8) {
+            ph[e] = static_cast<_Float16>(w[8 * u + e] * vs[u][half]);
+          } else {
+            pf[e] = static_cast<__bf16>(w[8 * u + e]);
+            pl[e] = static_cast<__bf16>(w[8 * u + e] - static_cast<float>(pf[e]));
+          }
+        }
 #pragma unroll
         for (int b = 0; b < T::DB; ++b) {
-          bf16x8 vf;
+          f32x16& ob = o[half * T::DB + b];
           if constexpr (FP8) {
             // source lane (k, a) = (ri / 2, ri % 2): key 16 u + 8 h + k, dims 32 b + 16 (grp & 1) + 8 a
             const int Rv = 16 * u + 8 * h + (ri >> 1);
             const int dbyte = 32 * b + 16 * (grp & 1) + 8 * (ri & 1);
             const int off = Rv * T::RB + 16 * ((dbyte >> 4) ^ v_swz8<T::RB>(Rv)) + (dbyte & 15);
             const i32x2 raw = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)(vt + off));
-            vf = fp8x8_bf16x8(u32x2{static_cast<uint32_t>(raw.x), static_cast<uint32_t>(raw.y)});
+            ob = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+                fp8x8_f16x8(u32x2{static_cast<uint32_t>(raw.x), static_cast<uint32_t>(raw.y)}), ph, ob, 0, 0, 0);
           } else {
             const int kq = ri >> 2, a = ri & 3;
             const int chunk = 4 * b + 2 * (grp & 1) + (a >> 1);
@@ -317,9 +354,10 @@ __global__ __launch_bounds__(64) void diff_decode_kernel(DiffParams dp, PlanArg<
               const int off = Rv * T::RB + 16 * (chunk ^ v_swz16<T::RB>(Rv)) + 8 * (a & 1);
               part[e4] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(vt + off));
             }
-            vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
+            const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
+            ob = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, ob, 0, 0, 0);
+            ob = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pl, ob, 0, 0, 0);
           }
-          o[half * T::DB + b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, o[half * T::DB + b], 0, 0, 0);
         }
       }
     }
@@ -345,6 +383,10 @@ __global__ __launch_bounds__(64) void diff_decode_kernel(DiffParams dp, PlanArg<
     }
   }
   wait_vmcnt<0>();  // no DMA may land in LDS after the wave has ended
+  if constexpr (FP8) {
+#pragma unroll
+    for (int b = 0; b < T::VB; ++b) o[b] *= vs_max[b / T::DB];
+  }
 
   if (has_new) {  // the new token's own key and value (bf16)
     float part = 0.f;

@@ -12,13 +12,17 @@
 // whose rows are widened into LDS with their page's scale, as the extend kernel does).
 // Softmax scale and running max enter the exponent in fp32, exp2(s c - m); the weights
 // are rounded to the operand type (bf16: 2^-8 relative at most) and their sum is taken
-// after that, so numerator and denominator agree.  The running max is raised only when a
+// after that, so numerator and denominator agree.  For bf16 pools that rounding is the
+// largest error besides the output's own (relative 2-norm 2.3e-3 in all, 1.7e-3 of it the
+// output's).  fp16 weights and values, converted in LDS, would be as exact as the output's
+// rounding, but took 17% (D = 64) to 25% (D = 128) more time.  The running max is raised only when a
 // half-row's weight sum passes 2^16 (or is not finite).
 //
 // Scores run 32 keys ahead of the values: while a block's weights are formed, the scores
 // of the next 32 keys are on the matrix cores.  So key tiles cover the 64 keys from 32
 // behind the value tile's start, and both rotate through two stages with one barrier per
-// 64 keys.  At D = 128 the two stages of both take 128 KB of LDS, one workgroup per CU.
+// 64 keys.  Tiles wholly in the prefix, and tiles wholly in the new tokens that all rows
+// see, run in loops without row checks and masks.  At D = 128 the two stages of both take 128 KB of LDS, one workgroup per CU.
 #include <hip/hip_runtime.h>
 
 #include "../cw_internal.h"
@@ -405,7 +409,7 @@ void diff_extend_kernel(DiffParams dp, PlanArg<AP> ap) {
     scores(kt, blk, s);
     weights(x, pf, lsum);
     if (__any(!(lsum <= kSumLimit))) {
-      const float mx = fmaxf(block_max(x), m_run);
+      const float mx = fmaxf(block_max(x) - kHeadroom, m_run);
       const float alpha = __builtin_amdgcn_exp2f(m_run - mx);
       m_run = mx;
       l_run *= alpha;
@@ -453,7 +457,7 @@ void diff_extend_kernel(DiffParams dp, PlanArg<AP> ap) {
       scores(lds_k1, 1, xa);
       mask(b0, xa);
       const float mx = block_max(xa);
-      if (mx != -INFINITY) m_run = mx;  // a row that sees none of these keys sees none of the item
+      if (mx != -INFINITY) m_run = mx - kHeadroom;  // a row that sees none of these keys sees none of the item
     }
   }
 

@@ -36,7 +36,7 @@ def _bound(inp, out, terms, weight, eps, after, single):
         root = np.sqrt((x * x).mean(-1, keepdims=True) + eps)
         rms = np.sqrt((dx * dx).mean(-1, keepdims=True))
         dy = 1.1 * np.abs(after * weight) / root * (dx + np.abs(x) * rms / root)
-    return dy + 2.0 ** -8 * np.abs(out) + 1e-6
+    return dy + 2.0 ** -8 * np.abs(out) + 1e-38
 
 
 def _inputs(lp, ls, pairs, g, d, page, dt, seed=3, norm=True):
@@ -184,6 +184,31 @@ def test_rising_scores_raise_the_running_max(d, dt):
     over = np.abs(out.cpu().double().numpy() - ref) / _bound(inp, ref, terms, weight, 1e-5, 0.6, single)
     assert float(terms["scores"].max()) > 40 and over.max() <= 1.0, over.max()
     assert heads == 2
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("where", ["all huge", "all tiny", "one prefix page huge", "a new token huge", "first tile tiny", "zeros"])
+def test_values_of_any_size(where, d):
+    """bf16 pools: values near the ends of bf16's range, alone and among others."""
+    print(f"\n[case] diff values {where} {d}", flush=True)
+    w, _, lam, weight = _inputs([300, 0, 70, 300], [90, 130, 33, 1], 1, 3, d, 16, "bf16", seed=66)
+    big, small = 2.0 ** 60, 2.0 ** -60
+    if where.startswith("all"):
+        w.v_pool *= big if where == "all huge" else small
+        w.v_new *= big if where == "all huge" else small
+    elif where == "one prefix page huge":
+        w.v_pool[int(w.block_table[0, 9]), 1] *= big
+    elif where == "a new token huge":
+        w.v_new[200, 0] *= big
+    elif where == "first tile tiny":
+        for j in range(4):
+            w.v_pool[int(w.block_table[0, j])] *= small
+    else:
+        w.v_pool[:, 0] = 0
+        w.v_new[:, 0] = 0
+    dw = to_gpu(w)
+    # without a norm (its mean of squares would pass fp32)
+    _check(w, dw, lam, None, f"diff values {where} {d}", after=1.0)
 
 
 def test_other_stream_shared_workspace_and_repeat():
