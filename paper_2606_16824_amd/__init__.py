@@ -487,38 +487,71 @@ def build_step_tables(prefix_lens, suffix_lens, free_pages, block_table, page_si
                       cu_rows=None, seq_ids=None, positions=None, slots=None, info=None, workspace=None) -> StepTables:
     """The step's new block-table entries (in place) and its tokens' index arrays, from int32
     lengths on the GPU (cw_build_step_tables); waits for nothing."""
-    num, t = len(prefix_lens), int(max_tokens)
+    t = int(max_tokens)
+    if not isinstance(prefix_lens, torch.Tensor) or prefix_lens.dim() != 1:
+        raise ValueError("prefix_lens must be a 1-D int32 tensor")
+    num = prefix_lens.shape[0]
     if t < 0:
         raise ValueError(f"max_tokens = {t} is negative")
-    i32, i64 = (torch.int32,), (torch.int64,)
-    _want(prefix_lens, "prefix_lens", i32, (num,))
-    _want(suffix_lens, "suffix_lens", i32, (num,))
-    if not isinstance(free_pages, torch.Tensor) or free_pages.dim() != 1 or free_pages.dtype != torch.int32:
-        raise ValueError("free_pages must be a 1-D int32 tensor")
-    if not isinstance(block_table, torch.Tensor) or block_table.dim() != 2 or block_table.dtype != torch.int32:
-        raise ValueError("block_table must be a 2-D int32 tensor [num_seqs, bt_stride]")
-    if block_table.shape[0] < num:
-        raise ValueError(f"block_table has {block_table.shape[0]} rows for {num} sequences")
-    dev = prefix_lens.device
-    new = lambda n, dt: torch.empty(n, dtype=dt, device=dev)
-    cu_rows = new(num + 1, torch.int32) if cu_rows is None else cu_rows
-    seq_ids = new(t, torch.int32) if seq_ids is None else seq_ids
-    positions = new(t, torch.int32) if positions is None else positions
-    slots = new(t, torch.int64) if slots is None else slots
-    info = new(3, torch.int64) if info is None else info
-    _want(cu_rows, "cu_rows", i32, (num + 1,))
-    _want(seq_ids, "seq_ids", i32, (t,))
-    _want(positions, "positions", i32, (t,))
-    _want(slots, "slots", i64, (t,))
-    _want(info, "info", i64, (3,))
-    if workspace is None and (nb := step_tables_workspace_bytes(num)) > 0:
-        workspace = _workspace(nb, dev, None)
-    _one_device(prefix_lens, suffix_lens, free_pages, block_table, cu_rows, seq_ids, positions, slots, info, workspace)
+    if cu_rows is None or seq_ids is None or positions is None or slots is None or info is None:
+        new = lambda n, dt: torch.empty(n, dtype=dt, device=prefix_lens.device)
+        cu_rows = new(num + 1, torch.int32) if cu_rows is None else cu_rows
+        seq_ids = new(t, torch.int32) if seq_ids is None else seq_ids
+        positions = new(t, torch.int32) if positions is None else positions
+        slots = new(t, torch.int64) if slots is None else slots
+        info = new(3, torch.int64) if info is None else info
+    nb = 0
+    if num > _TABLES_WITHOUT_WORKSPACE and workspace is None:
+        workspace = _workspace(step_tables_workspace_bytes(num), prefix_lens.device, None)
+    if workspace is not None:
+        nb = workspace.numel() * workspace.element_size()
+    dev = torch._C._cuda_getDevice()
+    if not _quick_tables(dev, num, t, prefix_lens, suffix_lens, free_pages, block_table, cu_rows, seq_ids, positions, slots,
+                         info):
+        i32, i64 = (torch.int32,), (torch.int64,)
+        _want(prefix_lens, "prefix_lens", i32, (num,))
+        _want(suffix_lens, "suffix_lens", i32, (num,))
+        if not isinstance(free_pages, torch.Tensor) or free_pages.dim() != 1 or free_pages.dtype != torch.int32:
+            raise ValueError("free_pages must be a 1-D int32 tensor")
+        if not isinstance(block_table, torch.Tensor) or block_table.dim() != 2 or block_table.dtype != torch.int32:
+            raise ValueError("block_table must be a 2-D int32 tensor [num_seqs, bt_stride]")
+        if block_table.shape[0] < num:
+            raise ValueError(f"block_table has {block_table.shape[0]} rows for {num} sequences")
+        _want(cu_rows, "cu_rows", i32, (num + 1,))
+        _want(seq_ids, "seq_ids", i32, (t,))
+        _want(positions, "positions", i32, (t,))
+        _want(slots, "slots", i64, (t,))
+        _want(info, "info", i64, (3,))
+        for x in (prefix_lens, suffix_lens, free_pages, block_table, cu_rows, seq_ids, positions, slots, info):
+            _dptr(x)
+        _one_device(prefix_lens, suffix_lens, free_pages, block_table, cu_rows, seq_ids, positions, slots, info)
     _check(library().cw_build_step_tables(
-        _dptr(prefix_lens), _dptr(suffix_lens), num, _dptr(free_pages), free_pages.numel(), int(page_size),
-        _dptr(block_table), block_table.shape[1], t, _dptr(cu_rows), _dptr(seq_ids), _dptr(positions), _dptr(slots),
-        _dptr(info), _dptr(workspace), 0 if workspace is None else workspace.numel(), _stream()))
+        prefix_lens.data_ptr(), suffix_lens.data_ptr(), num, free_pages.data_ptr(), free_pages.shape[0], int(page_size),
+        block_table.data_ptr(), block_table.shape[1], t, cu_rows.data_ptr(), seq_ids.data_ptr(), positions.data_ptr(),
+        slots.data_ptr(), info.data_ptr(), _dptr(workspace), nb, torch._C._cuda_getCurrentRawStream(dev)))
     return StepTables(cu_rows, seq_ids, positions, slots, info)
+
+
+_TABLES_WITHOUT_WORKSPACE = 4096  # cw_step_tables_workspace_bytes is 0 up to here
+
+
+def _quick_tables(dev, num, t, prefix_lens, suffix_lens, free_pages, block_table, cu_rows, seq_ids, positions, slots, info):
+    """Whether every check of build_step_tables passes (else they are made one at a time): the
+    call's own work takes 4 us on the GPU."""
+    i32, i64 = torch.int32, torch.int64
+    try:
+        for x, n in ((prefix_lens, num), (suffix_lens, num), (free_pages, -1), (cu_rows, num + 1), (seq_ids, t),
+                     (positions, t)):
+            if not (x.dtype is i32 and x.dim() == 1 and (x.shape[0] == n or n < 0) and x.get_device() == dev
+                    and x.is_contiguous()):
+                return False
+        for x, n in ((slots, t), (info, 3)):
+            if not (x.dtype is i64 and x.dim() == 1 and x.shape[0] == n and x.get_device() == dev and x.is_contiguous()):
+                return False
+        return (block_table.dtype is i32 and block_table.dim() == 2 and block_table.shape[0] >= num
+                and block_table.get_device() == dev and block_table.is_contiguous())
+    except AttributeError:
+        return False
 
 
 def _one_device(*tensors):
@@ -543,6 +576,77 @@ def _head_rows(t, name, total, heads, d):
     return t.data_ptr(), t.stride(0) if total > 1 else heads * d
 
 
+def _quick_rope(dev, total, hq, hkv, d, q, k, v, cos_sin, positions, weights, outs, k_pool, v_pool, slots, k_scale, v_scale):
+    """Whether every check of qk_norm_rope passes (else they are made one at a time)."""
+    try:
+        for x, h in ((q, hq), (k, hkv), (v, hkv)):
+            if x is None:
+                continue
+            s = x.stride()
+            if not (x.dtype is torch.bfloat16 and x.shape == (total, h, d) and s[2] == 1 and (s[1] == d or h == 1)
+                    and x.get_device() == dev):
+                return False
+        for x, h in outs:
+            if x is not None and not (x.dtype is torch.bfloat16 and x.shape == (total, h, d) and x.get_device() == dev
+                                      and x.is_contiguous()):
+                return False
+        if not (cos_sin.dtype is torch.float32 and cos_sin.dim() == 2 and cos_sin.get_device() == dev
+                and cos_sin.is_contiguous() and positions.dtype is torch.int32 and positions.shape == (total,)
+                and positions.get_device() == dev and positions.is_contiguous()):
+            return False
+        for x in weights:
+            if x is not None and not (x.dtype is torch.float32 and x.shape == (d,) and x.get_device() == dev
+                                      and x.is_contiguous()):
+                return False
+        if k_pool is None:
+            return v_pool is None and slots is None and k_scale is None and v_scale is None
+        shape, dt = k_pool.shape, k_pool.dtype
+        if not (len(shape) == 4 and shape[1] == hkv and shape[3] == d and v_pool.shape == shape and v_pool.dtype is dt
+                and k_pool.get_device() == dev and v_pool.get_device() == dev and k_pool.is_contiguous()
+                and v_pool.is_contiguous() and v is not None and slots.dtype is torch.int64 and slots.shape == (total,)
+                and slots.get_device() == dev and slots.is_contiguous()):
+            return False
+        if dt is torch.bfloat16:
+            return k_scale is None and v_scale is None
+        return dt in _FP8 and all(x.dtype is torch.float32 and x.shape == (shape[0], hkv) and x.get_device() == dev
+                                  and x.is_contiguous() for x in (k_scale, v_scale))
+    except (AttributeError, TypeError):
+        return False
+
+
+def _check_rope(total, hq, hkv, d, q, k, v, cos_sin, positions, q_weight, k_weight, q_out, k_out, v_out, k_pool, v_pool,
+                slots, k_scale, v_scale):
+    """The checks of qk_norm_rope, one at a time."""
+    for x, name, h in ((q, "q", hq), (k, "k", hkv), (v, "v", hkv)):
+        if x is not None:
+            _head_rows(x, name, total, h, d)
+    if not isinstance(cos_sin, torch.Tensor) or cos_sin.dim() != 2 or cos_sin.dtype != torch.float32:
+        raise ValueError("cos_sin must be a 2-D float32 tensor [positions, rotary_dim]")
+    _want(positions, "positions", (torch.int32,), (total,))
+    for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        if w is not None:
+            _want(w, name, (torch.float32,), (d,))
+    if k_pool is not None or v_pool is not None:
+        if k_pool is None or v_pool is None or v is None or slots is None:
+            raise ValueError("a page write needs k_pool, v_pool, slots and v")
+        _, pool_heads, _, pool_d = _check_pools(k_pool, v_pool, k_scale, v_scale)
+        if (pool_heads, pool_d) != (hkv, d):
+            raise ValueError(f"pools of {pool_heads} heads of {pool_d} for k of {hkv} heads of {d}")
+        _want(slots, "slots", (torch.int64,), (total,))
+    elif slots is not None or k_scale is not None or v_scale is not None:
+        raise ValueError("slots, k_scale and v_scale are for a page write (k_pool and v_pool)")
+    _want(q_out, "q_out", _BF16, (total, hq, d))
+    _want(k_out, "k_out", _BF16, (total, hkv, d))
+    if v_out is not None:
+        if v is None:
+            raise ValueError("v_out without v")
+        _want(v_out, "v_out", _BF16, (total, hkv, d))
+    for x in (cos_sin, positions, q_weight, k_weight, q_out, k_out, v_out, k_pool, v_pool, k_scale, v_scale, slots):
+        _dptr(x)
+    _one_device(q, k, v, cos_sin, positions, q_weight, k_weight, k_pool, v_pool, slots, k_scale, v_scale, q_out, k_out,
+                v_out)
+
+
 def qk_norm_rope(q, k, cos_sin, positions, q_weight=None, k_weight=None, eps=1e-6, interleaved=False, v=None,
                  k_pool=None, v_pool=None, slots=None, k_scale=None, v_scale=None, q_out=None, k_out=None, v_out=None):
     """Norm of every query and key head, position rotation and (with pools) page write in one
@@ -552,45 +656,28 @@ def qk_norm_rope(q, k, cos_sin, positions, q_weight=None, k_weight=None, eps=1e-
         raise ValueError("q and k must be 3-D tensors [T, heads, D]")
     total, hq, d = q.shape
     hkv = k.shape[1]
-    qp, qs = _head_rows(q, "q", total, hq, d)
-    kp, ks = _head_rows(k, "k", total, hkv, d)
-    vp, vs = (None, 0) if v is None else _head_rows(v, "v", total, hkv, d)
-    f32 = (torch.float32,)
-    if not isinstance(cos_sin, torch.Tensor) or cos_sin.dim() != 2 or cos_sin.dtype != torch.float32:
-        raise ValueError("cos_sin must be a 2-D float32 tensor [positions, rotary_dim]")
-    _want(positions, "positions", (torch.int32,), (total,))
-    for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-        if w is not None:
-            _want(w, name, f32, (d,))
-    num_pages, page, dt = 0, 0, L.CW_KV_BF16
-    if k_pool is not None or v_pool is not None:
-        if k_pool is None or v_pool is None or v is None or slots is None:
-            raise ValueError("a page write needs k_pool, v_pool, slots and v")
-        num_pages, pool_heads, page, pool_d = _check_pools(k_pool, v_pool, k_scale, v_scale)
-        if (pool_heads, pool_d) != (hkv, d):
-            raise ValueError(f"pools of {pool_heads} heads of {pool_d} for k of {hkv} heads of {d}")
-        _want(slots, "slots", (torch.int64,), (total,))
-        dt = _kv_dtype(k_pool)
-    elif slots is not None or k_scale is not None or v_scale is not None:
-        raise ValueError("slots, k_scale and v_scale are for a page write (k_pool and v_pool)")
     new = lambda h: torch.empty(total, h, d, dtype=torch.bfloat16, device=q.device)
     q_out = new(hq) if q_out is None else q_out
     k_out = new(hkv) if k_out is None else k_out
     if v is not None and v_out is None:
         v_out = new(hkv)
-    _want(q_out, "q_out", _BF16, (total, hq, d))
-    _want(k_out, "k_out", _BF16, (total, hkv, d))
-    if v_out is not None:
-        if v is None:
-            raise ValueError("v_out without v")
-        _want(v_out, "v_out", _BF16, (total, hkv, d))
-    _one_device(q, k, v, cos_sin, positions, q_weight, k_weight, k_pool, v_pool, slots, k_scale, v_scale, q_out, k_out,
-                v_out)
+    dev = torch._C._cuda_getDevice()
+    if not _quick_rope(dev, total, hq, hkv, d, q, k, v, cos_sin, positions, (q_weight, k_weight),
+                       ((q_out, hq), (k_out, hkv), (v_out, hkv)), k_pool, v_pool, slots, k_scale, v_scale) \
+            or (v_out is not None and v is None):
+        _check_rope(total, hq, hkv, d, q, k, v, cos_sin, positions, q_weight, k_weight, q_out, k_out, v_out, k_pool, v_pool,
+                    slots, k_scale, v_scale)
+    num_pages, page, dt = 0, 0, L.CW_KV_BF16
+    if k_pool is not None:
+        num_pages, _, page, _ = k_pool.shape
+        dt = _kv_dtype(k_pool)
+    ptr = lambda x: None if x is None else x.data_ptr()
+    step = lambda x, h: x.stride(0) if total > 1 else h * d
     _check(library().cw_qk_norm_rope(
-        qp, qs, kp, ks, vp, vs, total, hq, hkv, d, _dptr(q_weight), _dptr(k_weight), float(eps), _dptr(cos_sin),
-        cos_sin.shape[0], cos_sin.shape[1], int(bool(interleaved)), _dptr(positions), _dptr(q_out), _dptr(k_out),
-        _dptr(v_out), _dptr(k_pool), _dptr(v_pool), _dptr(k_scale), _dptr(v_scale), _dptr(slots), num_pages, page, dt,
-        _stream()))
+        q.data_ptr(), step(q, hq), k.data_ptr(), step(k, hkv), ptr(v), 0 if v is None else step(v, hkv), total, hq, hkv, d,
+        ptr(q_weight), ptr(k_weight), eps, cos_sin.data_ptr(), cos_sin.shape[0], cos_sin.shape[1], 1 if interleaved else 0,
+        positions.data_ptr(), q_out.data_ptr(), k_out.data_ptr(), ptr(v_out), ptr(k_pool), ptr(v_pool), ptr(k_scale),
+        ptr(v_scale), ptr(slots), num_pages, page, dt, torch._C._cuda_getCurrentRawStream(dev)))
     return q_out, k_out, v_out
 
 
@@ -613,14 +700,17 @@ def diff_attention(q, k_new, v_new, k_pool, v_pool, block_table, prefix_lens, su
                                             k_scale, v_scale)
     if heads % 2:
         raise ValueError(f"pools of {heads} heads: differential attention takes pairs of them")
-    hp = heads // 2 * gqa_group
+    hp = heads // 2 * int(gqa_group)
+    if out is None:
+        out = torch.empty(total, hp, 2 * d, dtype=torch.bfloat16, device=q.device)
     _want(lam, "lam", (torch.float32,), (hp,))
     if norm_weight is not None:
         _want(norm_weight, "norm_weight", (torch.float32,), (2 * d,))
-    if out is None:
-        out = torch.empty(total, hp, 2 * d, dtype=torch.bfloat16, device=q.device)
     _want(out, "out", _BF16, (total, hp, 2 * d))
-    _one_device(q, lam, norm_weight, out)
+    dev = torch._C._cuda_getDevice()
+    if not (q.get_device() == dev == lam.get_device() == out.get_device()
+            and (norm_weight is None or norm_weight.get_device() == dev)):
+        _one_device(q, lam, norm_weight, out)
     if workspace is None:
         workspace = _workspace(diff_workspace_bytes(lp, ls, heads // 2, gqa_group, d, page, _kv_dtype(k_pool)),
                                q.device, None)

@@ -1413,7 +1413,7 @@ cw_status_t cw_build_step_tables(const int32_t* prefix_lens, const int32_t* suff
     p.sums = static_cast<int32_t*>(workspace);
     p.num_seqs = num_seqs;
     p.num_free = num_free;
-    p.page_size = page_size;
+    p.page_shift = page_size == 16 ? 4 : 6;
     p.bt_stride = bt_stride;
     p.max_tokens = max_tokens;
     const hipError_t e = launch_step_tables(p, stream);

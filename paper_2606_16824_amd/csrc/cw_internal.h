@@ -186,7 +186,7 @@ struct StepTablesParams {
   int32_t* sums;              // workspace, 2 (num_seqs + 1), above kStepTablesLdsSeqs sequences
   int32_t num_seqs;
   int32_t num_free;
-  int32_t page_size;
+  int32_t page_shift;  // log2 of the page size
   int32_t bt_stride;
   int32_t max_tokens;
 };

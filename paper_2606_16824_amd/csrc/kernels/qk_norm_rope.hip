@@ -10,9 +10,10 @@
 // one that the page write of k_out and v_out makes.
 //
 // Bound by memory: q, k and v are read and written once, in 16-byte pieces; D / 8 lanes
-// hold a head, so a wave works on 64 / (D / 8) heads at a time.  A wave keeps the angles
-// of its token in registers (64 bytes of them per 16 bytes of a head) over all the heads
-// that it takes.
+// hold a head, so a wave works on 64 / (D / 8) heads at a time.  A wave keeps its token's
+// angles times the weights in registers over all heads that it takes (64 bytes of them
+// per 16 bytes of a head: read for each head they took a third of the loads), and issues
+// the loads of kBatch heads of each lane before it uses them.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -28,6 +29,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kThreads = 256;
+constexpr int kBatch = 4;  // heads of a lane whose loads are in flight together
 
 __device__ __forceinline__ float bf16_at(u32x4 x, int e) {
   return __uint_as_float(e % 2 ? x[e / 2] & 0xFFFF0000u : x[e / 2] << 16);
@@ -61,31 +63,35 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_kernel(NormRopeParams p
   const int per = (steps + p.splits - 1) / p.splits;
   const int s0 = (item % p.splits) * per, s1 = min(s0 + per, steps);
 
-  // this lane's angles, and for pairs i, i + R / 2 the lane that holds the other half
-  const int half = p.rot / 2, rot_lanes = p.rot / 8;
-  const bool turns = c < rot_lanes;
-  float cs[8], sn[8];  // interleaved: the first four
+  // this lane's angles, and for pairs i, i + R / 2 the lane that holds the other half: element
+  // e becomes r (x[e] w[e] cs[e] + x[other] w[other] sn[e]); lanes behind the rotated
+  // elements have cs = 1 and nothing to add
+  const int half = p.rot / 2;
+  const bool turns = 8 * c < p.rot;
+  float cs[8], sn[8];
   int partner = c;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) cs[e] = sn[e] = 0.f;
+  for (int e = 0; e < 8; ++e) {
+    cs[e] = 1.f;
+    sn[e] = 0.f;
+  }
   if (turns) {
     const float* row = p.cos_sin + size_t(pos) * p.rot;
     if constexpr (INTER) {
       const f32x4 a = *reinterpret_cast<const f32x4*>(row + 4 * c), b = *reinterpret_cast<const f32x4*>(row + half + 4 * c);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        cs[e] = a[e];
-        sn[e] = b[e];
+      for (int e = 0; e < 8; ++e) {
+        cs[e] = a[e / 2];
+        sn[e] = e % 2 ? b[e / 2] : -b[e / 2];
       }
     } else {
-      const int at = 8 * c < half ? 8 * c : 8 * c - half;
+      const bool first = 8 * c < half;  // of its pairs
+      const int at = first ? 8 * c : 8 * c - half;
       load8(cs, row + at);
       load8(sn, row + half + at);
-      partner = 8 * c < half ? c + half / 8 : c - half / 8;
-      if (8 * c < half) {
+      partner = first ? c + half / 8 : c - half / 8;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sn[e] = -sn[e];  // own cos + other (-sin): the first of a pair
-      }
+      for (int e = 0; e < 8; ++e) sn[e] = first ? -sn[e] : sn[e];
     }
   }
   const int64_t slot = POOL != 0 ? p.slots[tok] : -1;
@@ -93,72 +99,89 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_kernel(NormRopeParams p
   const int64_t page = paged ? slot / p.page_size : 0;
   const int in_page = paged ? static_cast<int>(slot % p.page_size) : 0;
 
-  for (int s = s0; s < s1; ++s) {
-    const int hd = s * RPW + lane / CH;
-    const bool is_q = hd < p.hq, is_k = !is_q && hd < p.hq + p.hkv;
-    const bool ok = hd < heads;
-    const int h = is_q ? hd : is_k ? hd - p.hq : hd - p.hq - p.hkv;
-    const uint16_t* src = static_cast<const uint16_t*>(is_q ? p.q : is_k ? p.k : p.v) +
-                          tok * (is_q ? p.q_stride : is_k ? p.k_stride : p.v_stride) + h * D + 8 * c;
-    u32x4 x = u32x4{0u, 0u, 0u, 0u};
-    if (ok) x = *reinterpret_cast<const u32x4*>(src);
-    u32x4 y = x;
-    const float* w = is_q ? p.q_weight : p.k_weight;
-    const bool norm = w != nullptr;
-    float r = 1.f;
-    {
-      float ss = 0.f;
+  // the factors of x[e] and of its partner for this lane's kind of head
+  float fa[8], fb[8];
+  int kind = -1;  // 0 a query head, 1 a key head, 2 a value head
+  bool norm = false;
+  auto kind_of = [&](int hd) { return hd < p.hq ? 0 : hd < p.hq + p.hkv ? 1 : 2; };
+
+  for (int sb = s0; sb < s1; sb += kBatch) {
+    u32x4 xs[kBatch];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) ss = fmaf(bf16_at(x, e), bf16_at(x, e), ss);
-#pragma unroll
-      for (int m = 1; m < CH; m <<= 1) ss += __shfl_xor(ss, m);
-      if (norm) r = 1.f / sqrtf(ss * (1.f / D) + p.eps);
+    for (int u = 0; u < kBatch; ++u) {
+      const int hd = (sb + u) * RPW + lane / CH;
+      xs[u] = u32x4{0u, 0u, 0u, 0u};
+      if (sb + u < s1 && hd < heads) {
+        const int kd = kind_of(hd);
+        const int h = kd == 0 ? hd : kd == 1 ? hd - p.hq : hd - p.hq - p.hkv;
+        const uint16_t* src = static_cast<const uint16_t*>(kd == 0 ? p.q : kd == 1 ? p.k : p.v) +
+                              tok * (kd == 0 ? p.q_stride : kd == 1 ? p.k_stride : p.v_stride) + h * D + 8 * c;
+        xs[u] = *reinterpret_cast<const u32x4*>(src);
+      }
     }
-    u32x4 other = x;
-    if constexpr (!INTER) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) other[e] = __shfl(x[e], (lane & ~(CH - 1)) | partner);
-    }
-    if (ok && (is_q || is_k)) {
-      float f[8], wt[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) wt[e] = 1.f;
-      if (norm) load8(wt, w + 8 * c);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) f[e] = bf16_at(x, e) * r * wt[e];
-      bf16x8 o;
-      if constexpr (INTER) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float a = f[2 * e], b = f[2 * e + 1];
-          o[2 * e] = static_cast<__bf16>(turns ? a * cs[e] - b * sn[e] : a);
-          o[2 * e + 1] = static_cast<__bf16>(turns ? b * cs[e] + a * sn[e] : b);
-        }
-      } else {
-        float wo[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) wo[e] = 1.f;
-        if (norm) load8(wo, w + 8 * partner);
+    for (int u = 0; u < kBatch; ++u) {
+      if (sb + u >= s1) break;  // (uniform)
+      const int hd = (sb + u) * RPW + lane / CH;
+      const int kd = kind_of(hd);
+      const int h = kd == 0 ? hd : kd == 1 ? hd - p.hq : hd - p.hq - p.hkv;
+      if (__any(kd != kind)) {  // (once or twice per token: another kind's weights)
+        kind = kd;
+        const float* w = kd == 0 ? p.q_weight : p.k_weight;
+        norm = w != nullptr && kd < 2;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const float g = bf16_at(other, e) * r * wo[e];
-          o[e] = static_cast<__bf16>(turns ? f[e] * cs[e] + g * sn[e] : f[e]);
+          fa[e] = cs[e];
+          fb[e] = sn[e];
+        }
+        if (norm) {
+          float wt[8], wo[8];
+          load8(wt, w + 8 * c);
+          load8(wo, w + 8 * partner);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            fa[e] *= wt[e];
+            fb[e] *= INTER ? wt[e ^ 1] : wo[e];
+          }
         }
       }
-      y = __builtin_bit_cast(u32x4, o);
-    }
-    if (!ok) continue;
-    uint16_t* out = static_cast<uint16_t*>(is_q ? p.q_out : is_k ? p.k_out : p.v_out);
-    if (out != nullptr)
-      *reinterpret_cast<u32x4*>(out + (int64_t(tok) * (is_q ? p.hq : p.hkv) + h) * D + 8 * c) = y;
-    if (POOL != 0 && paged && !is_q) {
-      const int64_t at = ((page * p.hkv + h) * p.page_size + in_page) * D + 8 * c;
-      void* pool = is_k ? p.k_pool : p.v_pool;
-      if constexpr (POOL == 2) {
-        const float sc = (is_k ? p.k_scale : p.v_scale)[page * p.hkv + h];
-        *reinterpret_cast<pw::u32x2*>(static_cast<uint8_t*>(pool) + at) = pw::quantise8(y, sc);
-      } else {
-        *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(pool) + at) = y;
+      const u32x4 x = xs[u];
+      float r = 1.f;
+      {
+        float ss = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) ss = fmaf(bf16_at(x, e), bf16_at(x, e), ss);
+#pragma unroll
+        for (int m = 1; m < CH; m <<= 1) ss += __shfl_xor(ss, m);
+        if (norm) r = 1.f / sqrtf(ss * (1.f / D) + p.eps);
+      }
+      u32x4 other = x;  // what the partner elements are read from
+      if constexpr (!INTER) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) other[e] = __shfl(x[e], (lane & ~(CH - 1)) | partner);
+      }
+      if (!turns) other = u32x4{0u, 0u, 0u, 0u};
+      u32x4 y = x;
+      if (kd < 2) {
+        bf16x8 o;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          o[e] = static_cast<__bf16>((bf16_at(x, e) * fa[e] + bf16_at(other, INTER ? e ^ 1 : e) * fb[e]) * r);
+        y = __builtin_bit_cast(u32x4, o);
+      }
+      if (hd >= heads) continue;
+      uint16_t* out = static_cast<uint16_t*>(kd == 0 ? p.q_out : kd == 1 ? p.k_out : p.v_out);
+      if (out != nullptr)
+        *reinterpret_cast<u32x4*>(out + (int64_t(tok) * (kd == 0 ? p.hq : p.hkv) + h) * D + 8 * c) = y;
+      if (POOL != 0 && paged && kd != 0) {
+        const int64_t at = ((page * p.hkv + h) * p.page_size + in_page) * D + 8 * c;
+        void* pool = kd == 1 ? p.k_pool : p.v_pool;
+        if constexpr (POOL == 2) {
+          const float sc = (kd == 1 ? p.k_scale : p.v_scale)[page * p.hkv + h];
+          *reinterpret_cast<pw::u32x2*>(static_cast<uint8_t*>(pool) + at) = pw::quantise8(y, sc);
+        } else {
+          *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(pool) + at) = y;
+        }
       }
     }
   }
