@@ -576,27 +576,31 @@ def _head_rows(t, name, total, heads, d):
     return t.data_ptr(), t.stride(0) if total > 1 else heads * d
 
 
-def _quick_rope(dev, total, hq, hkv, d, q, k, v, cos_sin, positions, weights, outs, k_pool, v_pool, slots, k_scale, v_scale):
+def _quick_rope(dev, total, hq, hkv, d, q, k, v, cos_sin, positions, weights, q_out, k_out, v_out, k_pool, v_pool, slots,
+                k_scale, v_scale):
     """Whether every check of qk_norm_rope passes (else they are made one at a time)."""
+    bf, f32 = torch.bfloat16, torch.float32
+    rows_q, rows = (total, hq, d), (total, hkv, d)
     try:
-        for x, h in ((q, hq), (k, hkv), (v, hkv)):
-            if x is None:
-                continue
-            s = x.stride()
-            if not (x.dtype is torch.bfloat16 and x.shape == (total, h, d) and s[2] == 1 and (s[1] == d or h == 1)
-                    and x.get_device() == dev):
+        _, q1, q2 = q.stride()
+        _, k1, k2 = k.stride()
+        if not (q.dtype is bf and q2 == 1 and (q1 == d or hq == 1) and q.get_device() == dev
+                and k.dtype is bf and k2 == 1 and (k1 == d or hkv == 1) and k.get_device() == dev and k.shape == rows
+                and q_out.dtype is bf and q_out.shape == rows_q and q_out.get_device() == dev and q_out.is_contiguous()
+                and k_out.dtype is bf and k_out.shape == rows and k_out.get_device() == dev and k_out.is_contiguous()
+                and cos_sin.dtype is f32 and cos_sin.dim() == 2 and cos_sin.get_device() == dev and cos_sin.is_contiguous()
+                and positions.dtype is torch.int32 and positions.shape == (total,) and positions.get_device() == dev
+                and positions.is_contiguous()):
+            return False
+        if v is not None:
+            _, v1, v2 = v.stride()
+            if not (v.dtype is bf and v2 == 1 and (v1 == d or hkv == 1) and v.get_device() == dev and v.shape == rows
+                    and v_out.dtype is bf and v_out.shape == rows and v_out.get_device() == dev and v_out.is_contiguous()):
                 return False
-        for x, h in outs:
-            if x is not None and not (x.dtype is torch.bfloat16 and x.shape == (total, h, d) and x.get_device() == dev
-                                      and x.is_contiguous()):
-                return False
-        if not (cos_sin.dtype is torch.float32 and cos_sin.dim() == 2 and cos_sin.get_device() == dev
-                and cos_sin.is_contiguous() and positions.dtype is torch.int32 and positions.shape == (total,)
-                and positions.get_device() == dev and positions.is_contiguous()):
+        elif v_out is not None:
             return False
         for x in weights:
-            if x is not None and not (x.dtype is torch.float32 and x.shape == (d,) and x.get_device() == dev
-                                      and x.is_contiguous()):
+            if x is not None and not (x.dtype is f32 and x.shape == (d,) and x.get_device() == dev and x.is_contiguous()):
                 return False
         if k_pool is None:
             return v_pool is None and slots is None and k_scale is None and v_scale is None
@@ -606,11 +610,13 @@ def _quick_rope(dev, total, hq, hkv, d, q, k, v, cos_sin, positions, weights, ou
                 and v_pool.is_contiguous() and v is not None and slots.dtype is torch.int64 and slots.shape == (total,)
                 and slots.get_device() == dev and slots.is_contiguous()):
             return False
-        if dt is torch.bfloat16:
+        if dt is bf:
             return k_scale is None and v_scale is None
-        return dt in _FP8 and all(x.dtype is torch.float32 and x.shape == (shape[0], hkv) and x.get_device() == dev
-                                  and x.is_contiguous() for x in (k_scale, v_scale))
-    except (AttributeError, TypeError):
+        pair = (shape[0], hkv)
+        return (dt in _FP8 and k_scale.dtype is f32 and k_scale.shape == pair and k_scale.get_device() == dev
+                and k_scale.is_contiguous() and v_scale.dtype is f32 and v_scale.shape == pair
+                and v_scale.get_device() == dev and v_scale.is_contiguous())
+    except (AttributeError, TypeError, ValueError):
         return False
 
 
@@ -656,28 +662,31 @@ def qk_norm_rope(q, k, cos_sin, positions, q_weight=None, k_weight=None, eps=1e-
         raise ValueError("q and k must be 3-D tensors [T, heads, D]")
     total, hq, d = q.shape
     hkv = k.shape[1]
-    new = lambda h: torch.empty(total, h, d, dtype=torch.bfloat16, device=q.device)
-    q_out = new(hq) if q_out is None else q_out
-    k_out = new(hkv) if k_out is None else k_out
-    if v is not None and v_out is None:
-        v_out = new(hkv)
+    if q_out is None or k_out is None or (v is not None and v_out is None):
+        new = lambda h: torch.empty(total, h, d, dtype=torch.bfloat16, device=q.device)
+        q_out = new(hq) if q_out is None else q_out
+        k_out = new(hkv) if k_out is None else k_out
+        v_out = new(hkv) if v is not None and v_out is None else v_out
     dev = torch._C._cuda_getDevice()
-    if not _quick_rope(dev, total, hq, hkv, d, q, k, v, cos_sin, positions, (q_weight, k_weight),
-                       ((q_out, hq), (k_out, hkv), (v_out, hkv)), k_pool, v_pool, slots, k_scale, v_scale) \
-            or (v_out is not None and v is None):
+    if not _quick_rope(dev, total, hq, hkv, d, q, k, v, cos_sin, positions, (q_weight, k_weight), q_out, k_out, v_out,
+                       k_pool, v_pool, slots, k_scale, v_scale):
         _check_rope(total, hq, hkv, d, q, k, v, cos_sin, positions, q_weight, k_weight, q_out, k_out, v_out, k_pool, v_pool,
                     slots, k_scale, v_scale)
+    vp = vs = vo = kp = vpool = sl = ks = vsc = None
     num_pages, page, dt = 0, 0, L.CW_KV_BF16
+    if v is not None:
+        vp, vs, vo = v.data_ptr(), v.stride(0) if total > 1 else hkv * d, v_out.data_ptr()
     if k_pool is not None:
         num_pages, _, page, _ = k_pool.shape
-        dt = _kv_dtype(k_pool)
-    ptr = lambda x: None if x is None else x.data_ptr()
-    step = lambda x, h: x.stride(0) if total > 1 else h * d
+        kp, vpool, sl = k_pool.data_ptr(), v_pool.data_ptr(), slots.data_ptr()
+        if k_scale is not None:
+            dt, ks, vsc = L.CW_KV_FP8_E4M3FN, k_scale.data_ptr(), v_scale.data_ptr()
     _check(library().cw_qk_norm_rope(
-        q.data_ptr(), step(q, hq), k.data_ptr(), step(k, hkv), ptr(v), 0 if v is None else step(v, hkv), total, hq, hkv, d,
-        ptr(q_weight), ptr(k_weight), eps, cos_sin.data_ptr(), cos_sin.shape[0], cos_sin.shape[1], 1 if interleaved else 0,
-        positions.data_ptr(), q_out.data_ptr(), k_out.data_ptr(), ptr(v_out), ptr(k_pool), ptr(v_pool), ptr(k_scale),
-        ptr(v_scale), ptr(slots), num_pages, page, dt, torch._C._cuda_getCurrentRawStream(dev)))
+        q.data_ptr(), q.stride(0) if total > 1 else hq * d, k.data_ptr(), k.stride(0) if total > 1 else hkv * d, vp, vs or 0,
+        total, hq, hkv, d, None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr(),
+        eps, cos_sin.data_ptr(), cos_sin.shape[0], cos_sin.shape[1], 1 if interleaved else 0, positions.data_ptr(),
+        q_out.data_ptr(), k_out.data_ptr(), vo, kp, vpool, ks, vsc, sl, num_pages, page, dt,
+        torch._C._cuda_getCurrentRawStream(dev)))
     return q_out, k_out, v_out
 
 

@@ -104,10 +104,8 @@ template <int D, int P, bool FP8, int AP>
 __global__ __launch_bounds__(64) void diff_decode_kernel(DiffParams dp, PlanArg<AP> ap) {
   using T = Geo<D, P, FP8>;
   const ExtendParams& p = dp.a;
-  // one array per stage: every step addresses a fixed array
-  __shared__ __attribute__((aligned(1024))) uint8_t lds_s0[T::TILE];
-  __shared__ __attribute__((aligned(1024))) uint8_t lds_s1[T::TILE];
-  __shared__ __attribute__((aligned(1024))) uint8_t lds_s2[T::STAGES > 2 ? T::TILE : 16];
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[T::STAGES * T::TILE];  // stages, then O
+  __shared__ float sh_row[3][32];  // per column: l, and the factors of its O and of the new value
 
   WorkItem it;
   if constexpr (AP != kPlanInMemory) {  // the plan in the kernel arguments, in compact form
@@ -178,8 +176,9 @@ __global__ __launch_bounds__(64) void diff_decode_kernel(DiffParams dp, PlanArg<
 
   // Q^T (B operand): this column's query, the other map's operand zero.  bf16 pools: k-step
   // kk holds dims 16 kk + 8 h + e; fp8 pools read 16 dims per fragment, so k-steps 2 t and 2
-  // t + 1 hold dims 32 t + 16 h + 8 (kk & 1) + e.  And the new token's key and value, used
-  // after the last tile, read here so that their latency does not end the item.
+  // t + 1 hold dims 32 t + 16 h + 8 (kk & 1) + e.  And the new token's key, and what each lane
+  // needs at the end (values lane * PER on of a row), read here so that their latency does
+  // not end the item.
   auto dim0 = [&](int kk) { return FP8 ? 32 * (kk >> 1) + 16 * h + 8 * (kk & 1) : 16 * kk + 8 * h; };
   bf16x8 qf[2][T::KT];
   {
@@ -195,17 +194,19 @@ __global__ __launch_bounds__(64) void diff_decode_kernel(DiffParams dp, PlanArg<
     }
   }
   bf16x8 k_own[T::KT];
-  bf16x4 v_own[T::VB][4];
+  constexpr int PER = 2 * D / 64;
+  typedef float fvec __attribute__((ext_vector_type(PER)));
+  typedef uint16_t hvec __attribute__((ext_vector_type(PER)));
+  const int d0 = lane * PER;
+  hvec v_own = hvec(0);
+  fvec wt = fvec(1.f);
   if (has_new) {
     const uint16_t* kn = static_cast<const uint16_t*>(p.k_new) + (size_t(tok) * hkv + 2 * pair + map) * D;
-    const uint16_t* vn = static_cast<const uint16_t*>(p.v_new) + (size_t(tok) * hkv + 2 * pair) * D;  // both halves
 #pragma unroll
     for (int kk = 0; kk < T::KT; ++kk) k_own[kk] = *reinterpret_cast<const bf16x8*>(kn + dim0(kk));
-#pragma unroll
-    for (int b = 0; b < T::VB; ++b)
-#pragma unroll
-      for (int q4 = 0; q4 < 4; ++q4) v_own[b][q4] = *reinterpret_cast<const bf16x4*>(vn + 32 * b + 8 * q4 + 4 * h);
+    v_own = *reinterpret_cast<const hvec*>(static_cast<const uint16_t*>(p.v_new) + (size_t(tok) * hkv + 2 * pair) * D + d0);
   }
+  if (it.part < 0 && dp.weight != nullptr) wt = *reinterpret_cast<const fvec*>(dp.weight + d0);
 
   // DMA of tile t: instruction j of a matrix covers tile rows [j RPI, (j + 1) RPI); rows past
   // the chunk's prefix end fetch its last key again (their scores are masked), so every tile
@@ -239,9 +240,9 @@ __global__ __launch_bounds__(64) void diff_decode_kernel(DiffParams dp, PlanArg<
   // Q, the new token's rows and the page ids land first (the addresses need the ids), so
   // only DMA is outstanding in the loop
   __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8));
-  if (n_tiles > 0) issue_tile(0, lds_addr(lds_s0));
-  if (n_tiles > 1) issue_tile(1, lds_addr(lds_s1));
-  if (T::STAGES > 2 && n_tiles > 2) issue_tile(2, lds_addr(lds_s2));
+  const uint32_t lds_base = lds_addr(lds);
+#pragma unroll 1
+  for (int t = 0; t < min(n_tiles, T::STAGES); ++t) issue_tile(t, lds_base + t * T::TILE);
 
   auto compute = [&](int t, const uint8_t* st) __attribute__((always_inline)) {
     const int j0 = kb + t * kKeys;
@@ -363,32 +364,30 @@ __global__ __launch_bounds__(64) void diff_decode_kernel(DiffParams dp, PlanArg<
     }
   };
   // Tile t lives in stage t % STAGES.  A step waits for its tile (those issued after it may
-  // still fly), computes on it, then refills the stage if there is a tile for it.
-  auto step = [&](int t, const uint8_t* st) __attribute__((always_inline)) {
+  // still fly), computes on it, then refills the stage if there is a tile for it.  One copy
+  // of the code for all stages: a short call runs through it cold, and fetching its
+  // instructions is a large part of its time (unrolled by the stages, with O exchanged and
+  // the new value added in registers, a decode of one token alone took 13.8 us at D = 128
+  // and of 1700 keys 15.7 us, against 5.3 and 11.2 us).
+  uint32_t off = 0;
+#pragma unroll 1
+  for (int t = 0; t < n_tiles; ++t) {
     const int behind = n_tiles - 1 - t;
     if (T::STAGES > 2 && behind >= 2) wait_vmcnt<(T::STAGES - 1) * T::DMA>();
     else if (behind >= 1) wait_vmcnt<T::DMA>();
     else wait_vmcnt<0>();
-    compute(t, st);
+    compute(t, lds + off);
     if (behind >= T::STAGES) {
       wait_lgkmcnt0();  // the stage's reads are done before it is refilled
-      issue_tile(t + T::STAGES, lds_addr(st));
+      issue_tile(t + T::STAGES, lds_base + off);
     }
-  };
-  for (int t = 0; t < n_tiles; t += T::STAGES) {
-    step(t, lds_s0);
-    if (t + 1 < n_tiles) step(t + 1, lds_s1);
-    if constexpr (T::STAGES > 2) {
-      if (t + 2 < n_tiles) step(t + 2, lds_s2);
-    }
+    off = off == (T::STAGES - 1) * T::TILE ? 0u : off + T::TILE;
   }
   wait_vmcnt<0>();  // no DMA may land in LDS after the wave has ended
-  if constexpr (FP8) {
-#pragma unroll
-    for (int b = 0; b < T::VB; ++b) o[b] *= vs_max[b / T::DB];
-  }
 
-  if (has_new) {  // the new token's own key and value (bf16)
+  // the new token's own key: its weight, and what it leaves of the others'
+  float left = 1.f, own = 0.f;
+  if (has_new) {
     float part = 0.f;
 #pragma unroll
     for (int kk = 0; kk < T::KT; ++kk) {
@@ -398,44 +397,64 @@ __global__ __launch_bounds__(64) void diff_decode_kernel(DiffParams dp, PlanArg<
     }
     const float x = row_sum(part) * c;
     const float m_new = fmaxf(m_run, x);
-    const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
-    const float pn = __builtin_amdgcn_exp2f(x - m_new);
+    left = __builtin_amdgcn_exp2f(m_run - m_new);
+    own = __builtin_amdgcn_exp2f(x - m_new);
     m_run = m_new;
-    l_run = l_run * alpha + (h == 0 ? pn : 0.f);
-#pragma unroll
-    for (int b = 0; b < T::VB; ++b)
-#pragma unroll
-      for (int q4 = 0; q4 < 4; ++q4)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          o[b][4 * q4 + e] = fmaf(pn, static_cast<float>(v_own[b][q4][e]), o[b][4 * q4 + e] * alpha);
   }
+  const float l_tot = fmaf(row_sum(l_run), left, own);
 
-  const float l_tot = row_sum(l_run);
-  if (it.part >= 0) {  // unnormalised partials of both maps, merged by diff_combine
-    if (!row_ok) return;
-    const size_t slot = size_t(it.part) * p.part_rows + map * (p.part_rows / 2) + g;
-    float* po = static_cast<float*>(p.part_o) + slot * (2 * D);
-#pragma unroll
-    for (int b = 0; b < T::VB; ++b)
-#pragma unroll
-      for (int q4 = 0; q4 < 4; ++q4)
-        *reinterpret_cast<f32x4*>(po + 32 * b + 8 * q4 + 4 * h) =
-            f32x4{o[b][4 * q4], o[b][4 * q4 + 1], o[b][4 * q4 + 2], o[b][4 * q4 + 3]};
-    if (h == 0) *reinterpret_cast<f32x2*>(p.part_ml + slot * 2) = f32x2{m_run, l_tot};
-    return;
-  }
-  // the second map's columns give lam O2 / l2 to the first map's (lanes l and l + 16)
-  const float f = (map == 0 ? 1.f : row_ok ? dp.lam[pair * G + g] : 0.f) / l_tot;
+  // O through LDS: a lane then holds PER consecutive values of a row.  Row `col` of the
+  // accumulators is left * O + own * v_new (fp8: O times its half's largest scale).
+  constexpr int ROW = 2 * D + 4;  // floats; the shift by 16 bytes spreads the columns over the banks
+  static_assert(32 * ROW * 4 <= T::STAGES * T::TILE, "O fits the stages");
+  float* const sh_o = reinterpret_cast<float*>(lds);
 #pragma unroll
   for (int b = 0; b < T::VB; ++b)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const float mine = o[b][i] * f;
-      o[b][i] = mine - __shfl_xor(mine, 16);
+    for (int q4 = 0; q4 < 4; ++q4)
+      *reinterpret_cast<f32x4*>(sh_o + col * ROW + 32 * b + 8 * q4 + 4 * h) =
+          f32x4{o[b][4 * q4], o[b][4 * q4 + 1], o[b][4 * q4 + 2], o[b][4 * q4 + 3]};
+  if (h == 0) {
+    sh_row[0][col] = l_tot;
+    sh_row[1][col] = left;
+    sh_row[2][col] = own;
+  }
+  __syncthreads();  // (one wave)
+  const float vs_half = vs_max[lane / 32];
+  fvec vn;
+#pragma unroll
+  for (int e = 0; e < PER; ++e) vn[e] = __uint_as_float(uint32_t(v_own[e]) << 16);
+  auto row = [&](int rc) -> fvec {
+    const fvec x = *reinterpret_cast<const fvec*>(sh_o + rc * ROW + d0);
+    return x * (sh_row[1][rc] * vs_half) + vn * sh_row[2][rc];
+  };
+  if (it.part >= 0) {  // unnormalised partials of both maps, merged by diff_combine
+    if (row_ok && h == 0)
+      *reinterpret_cast<f32x2*>(p.part_ml + (size_t(it.part) * p.part_rows + map * (p.part_rows / 2) + g) * 2) =
+          f32x2{m_run, l_tot};
+#pragma unroll 1
+    for (int i = 0; i < 2 * G; ++i) {
+      const int m = i < G ? 0 : 1, gi = i - m * G;
+      const size_t slot = size_t(it.part) * p.part_rows + m * (p.part_rows / 2) + gi;
+      *reinterpret_cast<fvec*>(static_cast<float*>(p.part_o) + slot * (2 * D) + d0) = row(16 * m + gi);
     }
-  if (map == 0 && row_ok)
-    store_row<T::VB>(dp, static_cast<uint16_t*>(p.out) + (size_t(tok) * hp + size_t(pair) * G + g) * (2 * D), h, o);
+    return;
+  }
+#pragma unroll 1
+  for (int gi = 0; gi < G; ++gi) {
+    const int head = pair * G + gi;
+    const fvec x = row(gi) * (1.f / sh_row[0][gi]) - row(16 + gi) * (dp.lam[head] / sh_row[0][16 + gi]);
+    float ss = 0.f;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) ss = fmaf(x[e], x[e], ss);
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) ss += __shfl_xor(ss, d);
+    const float f = row_factor(dp, ss, D);
+    hvec y;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) y[e] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(x[e] * f * wt[e]));
+    *reinterpret_cast<hvec*>(static_cast<uint16_t*>(p.out) + (size_t(tok) * hp + head) * (2 * D) + d0) = y;
+  }
 }
 
 template <int D, int P, bool FP8>
