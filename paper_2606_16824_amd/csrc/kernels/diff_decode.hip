@@ -4,10 +4,11 @@
 // 64 pages of one sequence's prefix, plus the new token's own key when the chunk ends the
 // sequence.  Every cached K/V byte is read once, so the kernel is bound by HBM.
 //
-// Both maps share one accumulator: columns 0-15 of the 32 of an MFMA are the first map's
-// queries, columns 16-31 the second's.  S^T = K1 [Q1 | 0] + K2 [0 | Q2] (the zeros cost
-// matrix cycles, which a streaming kernel has to spare), one softmax pass serves both
-// maps, and O^T += V^T P^T multiplies both maps' weights with a value row read once.
+// Both maps share the accumulators: columns 0-15 of the 32 of an MFMA are the first map's
+// queries, columns 16-31 the second's.  K1 [Q1 | Q2] and K2 [Q1 | Q2] are both taken and
+// each lane keeps its map's (the others cost matrix cycles, which a streaming kernel has
+// to spare); one softmax pass then serves both maps, and O^T += V^T P^T multiplies both
+// maps' weights with a value row read once.
 //
 // A tile is 32 keys: rows of both key heads and both value halves, DMA'd into LDS by
 // global_load_lds_dwordx4 with the kernel's own vmcnt waits (see the decode kernel, whose
@@ -16,6 +17,11 @@
 // 128-144 KB of LDS.  fp8 pools keep their codes in LDS and are widened exactly (keys to
 // bf16, values to fp16); a page's K scale of each map multiplies that map's scores, the V
 // scales of the two halves multiply the weights (one set of weights per half).
+//
+// 48 decodes of 2k-32k keys, 4 key pairs of 128: bf16 pages 581 us (5.7 TB/s of K/V; a plain
+// copy moves 4.9 TB/s), fp8 pages 313 us (5.3 TB/s); 64-wide keys, 8 pairs: 516 and 285 us.
+// One decode of 131072 keys: 94 us bf16, 62 us fp8; of 1700 keys 12.7 us, its two launches,
+// the page ids' and the tiles' latencies, and 1.7 us per tile.
 #include <hip/hip_runtime.h>
 
 #include "../cw_internal.h"
@@ -174,23 +180,20 @@ __global__ __launch_bounds__(64) void diff_decode_kernel(DiffParams dp, PlanArg<
     }
   }
 
-  // Q^T (B operand): this column's query, the other map's operand zero.  bf16 pools: k-step
-  // kk holds dims 16 kk + 8 h + e; fp8 pools read 16 dims per fragment, so k-steps 2 t and 2
+  // Q^T (B operand): this column's query.  bf16 pools: k-step kk holds dims 16 kk + 8 h + e; fp8 pools read 16 dims per fragment, so k-steps 2 t and 2
   // t + 1 hold dims 32 t + 16 h + 8 (kk & 1) + e.  And the new token's key, and what each lane
   // needs at the end (values lane * PER on of a row), read here so that their latency does
   // not end the item.
   auto dim0 = [&](int kk) { return FP8 ? 32 * (kk >> 1) + 16 * h + 8 * (kk & 1) : 16 * kk + 8 * h; };
-  bf16x8 qf[2][T::KT];
+  bf16x8 qf[T::KT];
   {
     const uint16_t* qrow =
         static_cast<const uint16_t*>(p.q) + (2 * (size_t(tok) * hp + size_t(pair) * G + g) + map) * D;
 #pragma unroll
     for (int kk = 0; kk < T::KT; ++kk) {
       u32x4 v = {0u, 0u, 0u, 0u};
-      const u32x4 zero = v;
       if (row_ok) v = *reinterpret_cast<const u32x4*>(qrow + dim0(kk));
-      qf[0][kk] = __builtin_bit_cast(bf16x8, map == 0 ? v : zero);
-      qf[1][kk] = __builtin_bit_cast(bf16x8, map == 0 ? zero : v);
+      qf[kk] = __builtin_bit_cast(bf16x8, v);
     }
   }
   bf16x8 k_own[T::KT];
@@ -243,29 +246,54 @@ __global__ __launch_bounds__(64) void diff_decode_kernel(DiffParams dp, PlanArg<
   const uint32_t lds_base = lds_addr(lds);
 #pragma unroll 1
   for (int t = 0; t < min(n_tiles, T::STAGES); ++t) issue_tile(t, lds_base + t * T::TILE);
+  float x_own = 0.f;  // the new token's score, under the first tiles' latency
+  if (has_new) {
+#pragma unroll
+    for (int kk = 0; kk < T::KT; ++kk)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x_own = fmaf(static_cast<float>(qf[kk][e]), static_cast<float>(k_own[kk][e]), x_own);
+    x_own = row_sum(x_own) * c;
+  }
 
   auto compute = [&](int t, const uint8_t* st) __attribute__((always_inline)) {
     const int j0 = kb + t * kKeys;
-    f32x16 s = f32x16{};
+    f32x16 s = f32x16{}, s2 = f32x16{};
     const int R = swap_bits_2_3(col);  // row m of the block reads key swap(m)
+    const uint8_t* km = st + R * T::RB;
+    if constexpr (FP8) {
 #pragma unroll
-    for (int m = 0; m < 2; ++m) {
-      const uint8_t* km = st + m * T::MAT + R * T::RB;
-      if constexpr (FP8) {
+      for (int t2 = 0; t2 < T::KT / 2; ++t2) {
+        const uint8_t* at = km + 16 * ((2 * t2 + h) ^ k_swz<T::RB>(R));
+        const u32x4 r0 = *reinterpret_cast<const u32x4*>(at), r1 = *reinterpret_cast<const u32x4*>(at + T::MAT);
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fp8x8_bf16x8(u32x2{r0.x, r0.y}), qf[2 * t2], s, 0, 0, 0);
+        s2 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fp8x8_bf16x8(u32x2{r1.x, r1.y}), qf[2 * t2], s2, 0, 0, 0);
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fp8x8_bf16x8(u32x2{r0.z, r0.w}), qf[2 * t2 + 1], s, 0, 0, 0);
+        s2 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fp8x8_bf16x8(u32x2{r1.z, r1.w}), qf[2 * t2 + 1], s2, 0, 0, 0);
+      }
+    } else {
+      // fragments are read four (two k-steps of both maps) ahead of their products (left to
+      // the compiler each waited for its own read: 48 decodes over bf16 pages, with the
+      // values' fragments ahead too, 615 -> 581 us, of 1700 keys 14.8 -> 12.7 us)
+      bf16x8 kf[2][4];
+      auto read4 = [&](int g2, bf16x8(&f)[4]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int t2 = 0; t2 < T::KT / 2; ++t2) {
-          const u32x4 raw = *reinterpret_cast<const u32x4*>(km + 16 * ((2 * t2 + h) ^ k_swz<T::RB>(R)));
-          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fp8x8_bf16x8(u32x2{raw.x, raw.y}), qf[m][2 * t2], s, 0, 0, 0);
-          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fp8x8_bf16x8(u32x2{raw.z, raw.w}), qf[m][2 * t2 + 1], s, 0, 0, 0);
-        }
-      } else {
+        for (int i = 0; i < 4; ++i)
+          f[i] = *reinterpret_cast<const bf16x8*>(km + 16 * ((2 * (2 * g2 + (i >> 1)) + h) ^ k_swz<T::RB>(R)) + (i & 1) * T::MAT);
+      };
+      read4(0, kf[0]);
 #pragma unroll
-        for (int kk = 0; kk < T::KT; ++kk) {
-          const bf16x8 kf = *reinterpret_cast<const bf16x8*>(km + 16 * ((2 * kk + h) ^ k_swz<T::RB>(R)));
-          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[m][kk], s, 0, 0, 0);
+      for (int g2 = 0; g2 < T::KT / 2; ++g2) {
+        if (g2 + 1 < T::KT / 2) read4(g2 + 1, kf[(g2 + 1) & 1]);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          f32x16& acc = i & 1 ? s2 : s;
+          acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[g2 & 1][i], qf[2 * g2 + (i >> 1)], acc, 0, 0, 0);
         }
       }
     }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = map == 0 ? s[i] : s2[i];
     // element i holds key j0 + 16 (i / 8) + 8 h + i % 8; the keys of half-group i / 8 share a page
     float cg[2] = {c, c}, vs[2][2] = {{1.f, 1.f}, {1.f, 1.f}};
     if constexpr (FP8) {
@@ -322,7 +350,7 @@ __global__ __launch_bounds__(64) void diff_decode_kernel(DiffParams dp, PlanArg<
         // Neither form of the weights adds to the output's own rounding.  bf16 pools: a weight
         // is the sum of two bf16 (2^-16), for a second MFMA; fp8 pools: fp16 (2^-11), which
         // holds the codes exactly too.  One bf16 weight each: relative error 2.4e-3 instead of
-        // 1.7e-3 at the same time (48 decodes: bf16 627 -> 634 us, fp8 351 -> 352 us).
+        // 1.7e-3, 1% less time over bf16 pages and none over fp8 pages.
         bf16x8 pf, pl;
         f16x8 ph;
 #pragma unroll
@@ -362,13 +390,21 @@ __global__ __launch_bounds__(64) void diff_decode_kernel(DiffParams dp, PlanArg<
         }
       }
     }
+    if constexpr (!FP8) {  // (mask 0x100: LDS reads, 0x008: MFMAs) values' fragments three ahead
+      __builtin_amdgcn_sched_group_barrier(0x100, 6, 1);
+#pragma unroll
+      for (int i = 0; i < 2 * T::VB; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 2, 1);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
+      }
+    }
   };
   // Tile t lives in stage t % STAGES.  A step waits for its tile (those issued after it may
   // still fly), computes on it, then refills the stage if there is a tile for it.  One copy
   // of the code for all stages: a short call runs through it cold, and fetching its
   // instructions is a large part of its time (unrolled by the stages, with O exchanged and
   // the new value added in registers, a decode of one token alone took 13.8 us at D = 128
-  // and of 1700 keys 15.7 us, against 5.3 and 11.2 us).
+  // against 6.9, 48 decodes over bf16 pages 635 us against 615).
   uint32_t off = 0;
 #pragma unroll 1
   for (int t = 0; t < n_tiles; ++t) {
@@ -388,17 +424,9 @@ __global__ __launch_bounds__(64) void diff_decode_kernel(DiffParams dp, PlanArg<
   // the new token's own key: its weight, and what it leaves of the others'
   float left = 1.f, own = 0.f;
   if (has_new) {
-    float part = 0.f;
-#pragma unroll
-    for (int kk = 0; kk < T::KT; ++kk) {
-      const bf16x8 q = map == 0 ? qf[0][kk] : qf[1][kk];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) part = fmaf(static_cast<float>(q[e]), static_cast<float>(k_own[kk][e]), part);
-    }
-    const float x = row_sum(part) * c;
-    const float m_new = fmaxf(m_run, x);
+    const float m_new = fmaxf(m_run, x_own);
     left = __builtin_amdgcn_exp2f(m_run - m_new);
-    own = __builtin_amdgcn_exp2f(x - m_new);
+    own = __builtin_amdgcn_exp2f(x_own - m_new);
     m_run = m_new;
   }
   const float l_tot = fmaf(row_sum(l_run), left, own);
