@@ -65,7 +65,8 @@ cw_status_t cw_build_step_tables(const int32_t* prefix_lens, const int32_t* suff
  *     a, b = i, i + R / 2, or with interleaved != 0: 2 i, 2 i + 1
  * in fp32, rounded once to bf16.  v is not changed.  With pools, token t's K (after
  * norm and rotation) and V go to slot slots[t] % P of page slots[t] / P, with exactly
- * the bytes that cw_kv_write_pages of k_out and v would put there.
+ * the bytes that cw_kv_write_pages of k_out and v would put there.  With a weight, mean(x^2)
+ * must be an fp32 number (a head's values below about 2^60).
  *
  * q bf16 [T, Hq, D], k and v bf16 [T, Hkv, D] with the heads of a token contiguous and
  * q_stride, k_stride, v_stride elements (multiples of 8) from one token to the next, so
@@ -116,7 +117,10 @@ cw_status_t cw_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int6
  * 1..512; out_scale finite, norm_eps finite and >= 0.  Sequences with one new token run on
  * the HBM-streaming kernel, the others on the matrix-core kernel, which over fp8 pools
  * computes in fp16: |code * scale| and every q, k_new and v_new value of such a call must
- * lie below 65504.  A NaN or infinity in a new token's value may reach the rows of earlier
+ * lie below 65504 (and is held to 2^-25 where it lies below 2^-14).  The streaming kernel has
+ * no such limit, but takes the V scales of the pages that a sequence's weight lies on to be
+ * within 2^20 of each other.  A scale may be 0 (a page of zeros).  With a norm, mean(x_h^2)
+ * must be an fp32 number: values below about 2^59.  A NaN or infinity in a new token's value may reach the rows of earlier
  * tokens of its sequence (their weight for it is zero); slots at or past a prefix's
  * end are never read.  Lengths, plan, capture, aliasing and errors as for
  * cw_step_attention; the timing events are not recorded.  Workspace:

@@ -180,10 +180,10 @@ __global__ __launch_bounds__(64) void diff_decode_kernel(DiffParams dp, PlanArg<
     }
   }
 
-  // Q^T (B operand): this column's query.  bf16 pools: k-step kk holds dims 16 kk + 8 h + e; fp8 pools read 16 dims per fragment, so k-steps 2 t and 2
-  // t + 1 hold dims 32 t + 16 h + 8 (kk & 1) + e.  And the new token's key, and what each lane
-  // needs at the end (values lane * PER on of a row), read here so that their latency does
-  // not end the item.
+  // Q^T (B operand): this column's query.  bf16 pools: k-step kk holds dims 16 kk + 8 h + e;
+  // fp8 pools read 16 dims per fragment, so k-steps 2 t and 2 t + 1 hold dims 32 t + 16 h +
+  // 8 (kk & 1) + e.  And the new token's key, and what each lane needs at the end (values
+  // lane * PER on of a row), read here so that their latency does not end the item.
   auto dim0 = [&](int kk) { return FP8 ? 32 * (kk >> 1) + 16 * h + 8 * (kk & 1) : 16 * kk + 8 * h; };
   bf16x8 qf[T::KT];
   {
@@ -308,9 +308,13 @@ __global__ __launch_bounds__(64) void diff_decode_kernel(DiffParams dp, PlanArg<
       }
     }
     if (j0 + kKeys > ke) {  // keys past the chunk's prefix end
+      // (the page scales first: a page's may be 0, and then -inf times it is no mask)
 #pragma unroll
-      for (int i = 0; i < 16; ++i)
+      for (int i = 0; i < 16; ++i) {
+        if constexpr (FP8) s[i] *= cg[i >> 3];
         if (j0 + 16 * (i >> 3) + 8 * h + (i & 7) >= ke) s[i] = -INFINITY;
+      }
+      if constexpr (FP8) cg[0] = cg[1] = 1.f;
     }
     // weights against the running max as it stands; raised only when a half-column's sum
     // passes kSumLimit (or is not finite, as on an item's first tile)

@@ -211,6 +211,43 @@ def test_values_of_any_size(where, d):
     _check(w, dw, lam, None, f"diff values {where} {d}", after=1.0)
 
 
+@pytest.mark.parametrize("d,page", [(64, 64), (128, 16)])
+def test_pages_of_zeros_have_scale_zero(d, page):
+    """fp8 pages whose largest value is 0 and so their scale: a whole prefix, and last pages that
+    are partly filled, of K, of V and of both."""
+    print(f"\n[case] diff scale zero {d} {page}", flush=True)
+    w, _, lam, weight = _inputs([300, 309, 300, 309, 5, 70], [1, 1, 1, 90, 1, 40], 2, 3, d, page, "fp8", seed=67)
+    last = lambda b: int(w.block_table[b, (int(w.spec.prefix_lens[b]) - 1) // page])
+    w.k_scale[last(0)] = 0
+    w.v_scale[last(1)] = 0
+    w.k_scale[last(2), 1] = w.v_scale[last(2), 2] = 0
+    w.k_scale[last(3)] = w.v_scale[last(3)] = 0
+    for b in (4, 5):
+        for j in range(-(-int(w.spec.prefix_lens[b]) // page)):
+            w.k_scale[int(w.block_table[b, j])] = w.v_scale[int(w.block_table[b, j])] = 0
+    _check(w, to_gpu(w), lam, weight, f"diff scale zero {d}")
+
+
+@pytest.mark.parametrize("d,page", [(64, 16), (128, 64)])
+def test_value_scales_far_apart(d, page):
+    """Single tokens over fp8 pages whose V scales lie up to 2^20 apart, with most of the weight
+    on a page of small values.  (Scores reach 116: 2^-16 of them from the dot products, 2^-9 in all, is
+    less than the bound's 2^-7 leaves beside fp16 weights.)"""
+    print(f"\n[case] diff value scales {d} {page}", flush=True)
+    lp = [900, 500, 37]
+    w, _, lam, weight = _inputs(lp, [1, 1, 1], 2, 3, d, page, "fp8", seed=68)
+    rng = np.random.default_rng(5)
+    for b in range(3):
+        n = -(-lp[b] // page)
+        for j in range(n):
+            w.v_scale[int(w.block_table[b, j])] *= float(2.0 ** -rng.integers(0, 17))
+        pg = int(w.block_table[b, n // 2])
+        w.k_scale[pg] *= 12.0
+        w.v_scale[pg] = 2.0 ** -23  # (scales are at most 0.1)
+    w.v_new *= 2.0 ** -20
+    _check(w, to_gpu(w), lam, None, f"diff value scales {d}", after=1.0)
+
+
 def test_other_stream_shared_workspace_and_repeat():
     print("\n[case] diff on another stream", flush=True)
     w, dw, lam, weight = _inputs([900, 40, 333], [1, 200, 3], 2, 3, 128, 16, "bf16", seed=12)
