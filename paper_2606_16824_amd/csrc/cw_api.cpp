@@ -1189,8 +1189,7 @@ cw_status_t diff_impl(const void* q, const void* k_new, const void* v_new, const
     std::fill(h, h + sp.off_ext_meta, uint8_t(0));
     if (!sp.ext.empty()) pack_plan_meta(sp.ext_plan, h + sp.off_ext_meta);
   };
-  const bool arg_plan =
-      arg_plans() && (sp.dec.empty() || (sp.ext.empty() && compact && compact_arg_fits(cu.bytes)));
+  const bool arg_plan = arg_plans() && (sp.dec.empty() || (compact && compact_arg_fits(cu.bytes)));
   const size_t whole_bytes = sp.off_ext_meta + sp.ext_plan.whole_meta_bytes + sp.dec_plan.whole_meta_bytes;
   return stage_and_launch(sp.meta_bytes, whole_bytes, ws, stream, [&](uint8_t* h) {
     head(h);

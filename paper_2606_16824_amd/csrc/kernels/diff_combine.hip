@@ -5,7 +5,8 @@
 // A row's 2 D values lie over one wave; WPR waves share its partials (four where there are
 // many: decodes of long prefixes) and meet in LDS.  Each wave issues the loads of kBatch
 // partials of both maps before it uses them.  Bound by reading the partials (fp32: the
-// difference cancels, so they are not rounded on the way).
+// difference cancels, so they are not rounded on the way): 67 MB of a 1024-token chunk's in
+// 15.2 us, 4.4 TB/s; those of a step's decodes in 4.3-4.8 us, mostly latency.
 #include <hip/hip_runtime.h>
 
 #include "../cw_internal.h"

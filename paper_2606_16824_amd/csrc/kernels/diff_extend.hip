@@ -15,14 +15,20 @@
 // after that, so numerator and denominator agree.  For bf16 pools that rounding is the
 // largest error besides the output's own (relative 2-norm 2.3e-3 in all, 1.7e-3 of it the
 // output's).  fp16 weights and values, converted in LDS, would be as exact as the output's
-// rounding, but took 17% (D = 64) to 25% (D = 128) more time.  The running max is raised only when a
-// half-row's weight sum passes 2^16 (or is not finite).
+// rounding, but took 17% (D = 64) to 25% (D = 128) more time.  The running max is raised
+// only when a half-row's weight sum passes 2^16 (or is not finite).
 //
 // Scores run 32 keys ahead of the values: while a block's weights are formed, the scores
 // of the next 32 keys are on the matrix cores.  So key tiles cover the 64 keys from 32
 // behind the value tile's start, and both rotate through two stages with one barrier per
 // 64 keys.  Tiles wholly in the prefix, and tiles wholly in the new tokens that all rows
-// see, run in loops without row checks and masks.  At D = 128 the two stages of both take 128 KB of LDS, one workgroup per CU.
+// see, run in loops without row checks and masks.  At D = 128 the two stages of both take
+// 128 KB of LDS, one workgroup per CU.
+//
+// Bound by the matrix cores: 4096 new tokens on 32768 cached ones, 8 key pairs of 4 query
+// pairs at D = 128, take 6.05 ms, 1159 TFLOP/s (a plain bf16 product of 8192^3 reaches 1214);
+// at D = 64 (half the matrix work per exponential) 1068 TFLOP/s; over fp8 pools, whose
+// rows are widened on the way, 1026 and 933.  (Cards differ by up to 10%.)
 #include <hip/hip_runtime.h>
 
 #include "../cw_internal.h"
