@@ -705,8 +705,11 @@ std::shared_ptr<const StepPlan> diff_plan(const int32_t* lp, const int32_t* ls, 
   const bool fp8 = kv_dtype == CW_KV_FP8_E4M3FN;
   const PlanKinds kinds{
       [&](const PlanEnv& env, const int32_t* lp_e, const int32_t* ls_e, int32_t n, const int32_t* cu, const int32_t* bt) {
+        int64_t kv_bytes = 0;  // K and V of both heads of every pair
+        for (int32_t b = 0; b < n; ++b)
+          kv_bytes += (int64_t(lp_e[b]) * (fp8 ? 1 : 2) + int64_t(ls_e[b]) * 2) * 4 * head_dim * num_pairs;
         return build_extend_plan(lp_e, ls_e, n, num_pairs, gqa_group, 2 * head_dim, DIFF_BLOCK_M, 1, env.cus, env.xcds,
-                                 env.tuning, cu, bt, 2);
+                                 env.tuning, cu, bt, 2, kv_bytes);
       },
       [&](const PlanEnv& env, const int32_t* lp_d, int32_t n, size_t meta_at, const int32_t* cu, const int32_t* bt) {
         return build_decode_plan(lp_d, n, num_pairs, gqa_group, 2 * head_dim, page_size, diff_decode_keys_per_tile(),

@@ -34,6 +34,7 @@ size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
 struct Tile {
   int32_t seq, kvh, q_row0, rows, kv_len, n_kt, n_pre;  // n_pre: key tiles wholly in the prefix
+  int64_t rate;                                         // cost of a prefix key tile
 };
 
 // Work of one (sequence, kv head), or a share of it: items [first, first + n) of
@@ -69,21 +70,41 @@ size_t launch_count(const std::vector<std::vector<T>>& queues) {
 
 // ---- levelled plans -------------------------------------------------------
 // The cost model, in hundredths of the time one workgroup takes for a prefix
-// key tile when all its rows are in use (1.7-2.2 us at head dim 128).  Fewer
+// key tile when all its rows are in use (extend kernel: 1.7-2.2 us at head dim 128).  Fewer
 // rows make a tile cheaper only down to the time its K/V take to arrive
 // (measured per tile, 256 workgroups, unshared K/V: 2.19 us with 256 rows, 1.94
 // with 192, 1.58 with 128, 1.53 with 32).  At head dim 64 the same units stand for
 // about half that time.  A tile past the prefix counts suffix_weight: right for one
 // that straddles the prefix's end or the diagonal, too much for one wholly among the
 // new tokens, which the kernel runs without masks like a prefix tile.
-constexpr int64_t kItemCost = 300;       // start-up and epilogue of a work item
-constexpr int64_t kMergeCost = 450;      // the merge kernel's launch and latency
-constexpr int64_t kMergePartCost = 2;    // per partial slot merged
-constexpr int64_t kMinGap = MIN_CHUNK_TILES * 100 + kItemCost;
-// What cutting tiles has to gain at least (about 55 us at head dim 128): calls of
-// 20-100 us lost 5-60 us to the merge and the larger plan when they were levelled.
-// Asked in full also of plans that have partials, and so a merge, already.
-constexpr int64_t kMinCutGain = 3000;
+struct Costs {
+  int64_t item;        // start-up and epilogue of a work item
+  int64_t merge;       // the merge kernel's launch and latency
+  int64_t merge_part;  // per partial slot merged
+  // What cutting tiles has to gain at least (extend kernel: about 55 us at head dim 128):
+  // calls of 20-100 us lost 5-60 us to the merge and the larger plan when they were levelled.
+  // Asked in full also of plans that have partials, and so a merge, already.
+  int64_t min_cut_gain;
+  int64_t max_bytes;       // of meta and partial slots of a plan whose tiles are cut
+  int64_t reorder_percent; // what another order of whole tiles has to gain
+  int64_t min_gap() const { return MIN_CHUNK_TILES * 100 + item; }
+};
+constexpr Costs kExtendCosts{300, 450, 2, 3000, kLevelTotalBytes, 4};
+// Differential attention: a key tile of 128 rows takes 2.8 us at head dim 128 and 1.5 at 64
+// (taken to be the same where fewer rows are in use); a partial slot holds both maps in fp32,
+// twice an extend's bytes.  With the extend kernel's figures (and its limit on bytes, that
+// of the static scratch array, which these calls do not use) 4 chunks of up to 1008 tokens
+// over fp8 pages took 2.92 ms instead of 2.70, 2 of up to 3318 938 us instead of 877, one of
+// 94 on 43k keys 182 instead of 166.
+constexpr Costs kDiffCosts{250, 300, 4, 1000, 3 * kLevelTotalBytes, 2};
+// Pieces of cut tiles read different keys at the same time, and with 128 rows a key tile is
+// staged once per 2.8 us and CU, 6 TB/s in all: what the XCDs' L2 no longer share has to come
+// from the memory-side cache.  Where the call's K/V does not fit it, pieces count up to twice
+// (less where a sequence and kv head has few tiles): 2 chunks of up to 1519 tokens on 50k
+// keys (410 MB) took 3.86 ms cut and 3.17 whole, 14 of up to 139 on 41k (290 MB) 1101 us and
+// 809; but 9 of up to 1222 on 26k (270 MB), few of them cut, 1357 us and 1426, and 14 of up to
+// 318 at one query pair per key pair (694 MB, three tiles each) 831 us and 930.
+constexpr int64_t kSharedKvBytes = int64_t(192) << 20;
 
 int64_t row_rate(int32_t rows) {
   constexpr int64_t rate[8] = {72, 72, 72, 72, 80, 89, 95, 100};
@@ -93,14 +114,14 @@ int64_t row_rate(int32_t rows) {
 // Key tiles [a, b) of a query tile.
 int64_t span_cost(const Tile& t, int64_t a, int64_t b, int64_t suffix_weight) {
   const int64_t pre = std::max<int64_t>(0, std::min<int64_t>(b, t.n_pre) - a), suf = (b - a) - pre;
-  return (pre * 100 + suf * suffix_weight) * row_rate(t.rows) / 100;
+  return (pre * 100 + suf * suffix_weight) * t.rate / 100;
 }
-int64_t tile_cost(const Tile& t, int64_t suffix_weight) {
-  return kItemCost + span_cost(t, 0, t.n_kt, suffix_weight);
+int64_t tile_cost(const Costs& c, const Tile& t, int64_t suffix_weight) {
+  return c.item + span_cost(t, 0, t.n_kt, suffix_weight);
 }
 // The last key tile up to which the tiles from `a` on cost at most `budget`.
 int64_t span_end(const Tile& t, int64_t a, int64_t budget, int64_t suffix_weight) {
-  const int64_t units = std::max<int64_t>(0, budget) * 100 / row_rate(t.rows);
+  const int64_t units = std::max<int64_t>(0, budget) * 100 / t.rate;
   const int64_t pre = std::max<int64_t>(0, t.n_pre - a);
   if (units < pre * 100) return a + units / 100;
   return a + pre + (units - pre * 100) / suffix_weight;
@@ -157,23 +178,24 @@ struct Left {  // a tile not placed yet, from key tile k0 on
 
 // Fills the slots (in order of the time they are free) up to `level` with `left`
 // in pieces of key ranges; returns the entries used up.
-size_t fill_slots(const std::vector<Tile>& tiles, std::vector<Left>& left, std::vector<Slots::Slot>& slots,
-                  size_t& next, int64_t level, int64_t wgt, std::vector<Piece>& out) {
+size_t fill_slots(const Costs& c, const std::vector<Tile>& tiles, std::vector<Left>& left,
+                  std::vector<Slots::Slot>& slots, size_t& next, int64_t level, int64_t wgt,
+                  std::vector<Piece>& out) {
   size_t i = 0;
   while (i < left.size() && next < slots.size()) {
     Slots::Slot& sl = slots[next];
     Left& l = left[i];
     const Tile& t = tiles[l.tile];
     const int64_t gap = level - sl.t;
-    const int64_t whole = kItemCost + span_cost(t, l.k0, t.n_kt, wgt);
+    const int64_t whole = c.item + span_cost(t, l.k0, t.n_kt, wgt);
     if (whole <= gap) {
       out.push_back(Piece{l.tile, l.k0, t.n_kt, sl.t});
       sl.t += whole;
       ++i;
       continue;
     }
-    if (gap >= kMinGap) {
-      const int64_t e = std::min<int64_t>(span_end(t, l.k0, gap - kItemCost, wgt), t.n_kt - MIN_CHUNK_TILES);
+    if (gap >= c.min_gap()) {
+      const int64_t e = std::min<int64_t>(span_end(t, l.k0, gap - c.item, wgt), t.n_kt - MIN_CHUNK_TILES);
       if (e - l.k0 >= MIN_CHUNK_TILES) {
         out.push_back(Piece{l.tile, l.k0, static_cast<int32_t>(e), sl.t});
         l.k0 = static_cast<int32_t>(e);
@@ -188,7 +210,7 @@ size_t fill_slots(const std::vector<Tile>& tiles, std::vector<Left>& left, std::
 // `level`: a queue takes whole tiles in the order of `owned` while they end by
 // `level`; what is left fills the slots in pieces of key ranges, its own queue's
 // slots first.  Returns false if something does not fit.
-bool level_queues(const std::vector<Tile>& tiles, const std::vector<std::vector<int32_t>>& owned,
+bool level_queues(const Costs& cm, const std::vector<Tile>& tiles, const std::vector<std::vector<int32_t>>& owned,
                   const std::vector<bool>& as_before, int64_t wgt, int64_t R, int64_t level,
                   std::vector<std::vector<Piece>>& queues) {
   const size_t X = owned.size();
@@ -209,7 +231,7 @@ bool level_queues(const std::vector<Tile>& tiles, const std::vector<std::vector<
     }
     Slots heap(R);
     for (const int32_t ti : owned[x]) {
-      const int64_t c = tile_cost(tiles[ti], wgt);
+      const int64_t c = tile_cost(cm, tiles[ti], wgt);
       if (heap.soonest() + c > level) {
         left[x].push_back(Left{ti, 0});
         continue;
@@ -219,13 +241,13 @@ bool level_queues(const std::vector<Tile>& tiles, const std::vector<std::vector<
     }
     slots[x] = std::move(heap.s);
     std::sort(slots[x].begin(), slots[x].end());
-    const size_t used = fill_slots(tiles, left[x], slots[x], next[x], level, wgt, queues[x]);
+    const size_t used = fill_slots(cm, tiles, left[x], slots[x], next[x], level, wgt, queues[x]);
     left[x].erase(left[x].begin(), left[x].begin() + static_cast<std::ptrdiff_t>(used));
   }
   std::vector<Left> rest;
   for (size_t x = 0; x < X; ++x) rest.insert(rest.end(), left[x].begin(), left[x].end());
   for (size_t x = 0; x < X && !rest.empty(); ++x) {
-    const size_t used = fill_slots(tiles, rest, slots[x], next[x], level, wgt, queues[x]);
+    const size_t used = fill_slots(cm, tiles, rest, slots[x], next[x], level, wgt, queues[x]);
     rest.erase(rest.begin(), rest.begin() + static_cast<std::ptrdiff_t>(used));
   }
   return rest.empty();
@@ -248,8 +270,9 @@ bool level_queues(const std::vector<Tile>& tiles, const std::vector<std::vector<
 // stay in registers without the cut): rounded to bf16 they raised the error of 10
 // replies against 64 bits by 1%, and in fp32 the times are the same (10 replies 688
 // against 693 us, the mixed steps within 2%).
-void level_plan(ExtendPlan& plan, const std::vector<Tile>& tiles, const std::vector<Bundle>& whole_bundles,
-                int64_t wgt, int64_t R, int32_t head_dim, std::vector<std::vector<WorkItem>>& queues) {
+void level_plan(const Costs& cm, ExtendPlan& plan, const std::vector<Tile>& tiles,
+                const std::vector<Bundle>& whole_bundles, int64_t wgt, int64_t R, int32_t head_dim, int32_t maps,
+                bool shared, std::vector<std::vector<WorkItem>>& queues) {
   const size_t X = queues.size();
   if (tiles.empty() || tiles.size() > size_t(kMaxLevelTiles)) return;
 
@@ -262,9 +285,9 @@ void level_plan(ExtendPlan& plan, const std::vector<Tile>& tiles, const std::vec
       costs.clear();
       for (const WorkItem& w : q) {
         Tile t{};
-        t.rows = w.rows;
+        t.rate = maps > 1 ? 100 : row_rate(w.rows);
         t.n_pre = plan.seqs[w.seq].lp / BLOCK_N;
-        costs.push_back(kItemCost + span_cost(t, w.kv_begin / BLOCK_N, (w.kv_end + BLOCK_N - 1) / BLOCK_N, wgt));
+        costs.push_back(cm.item + span_cost(t, w.kv_begin / BLOCK_N, (w.kv_end + BLOCK_N - 1) / BLOCK_N, wgt));
         sum += costs.back();
       }
       if (costs != last) {
@@ -274,7 +297,7 @@ void level_plan(ExtendPlan& plan, const std::vector<Tile>& tiles, const std::vec
       now = std::max(now, last_span);
     }
   }
-  if (plan.n_parts > 0) now += kMergeCost + kMergePartCost * plan.n_parts;
+  if (plan.n_parts > 0) now += cm.merge + cm.merge_part * plan.n_parts;
   const int64_t slots = static_cast<int64_t>(X) * R;
   if (sum / slots * 103 >= now * 100) return;
 
@@ -290,7 +313,7 @@ void level_plan(ExtendPlan& plan, const std::vector<Tile>& tiles, const std::vec
   for (const Bundle& wb : whole_bundles) {
     Bd bd{static_cast<int32_t>(wb.first), static_cast<int32_t>(wb.n), 0, 0, INT64_MAX};
     for (int32_t i = bd.t0; i < bd.t0 + bd.n; ++i) {
-      const int64_t c = tile_cost(tiles[i], wgt);
+      const int64_t c = tile_cost(cm, tiles[i], wgt);
       bd.cost += c;
       bd.longest = std::max(bd.longest, c);
       bd.shortest = std::min(bd.shortest, c);
@@ -323,7 +346,7 @@ void level_plan(ExtendPlan& plan, const std::vector<Tile>& tiles, const std::vec
       const bool reverse = bd->shortest * 2 < bd->longest;
       for (int32_t i = 0; i < bd->n; ++i) {
         owned[x].push_back(reverse ? bd->t0 + bd->n - 1 - i : bd->t0 + i);
-        costs.push_back(tile_cost(tiles[owned[x].back()], wgt));
+        costs.push_back(tile_cost(cm, tiles[owned[x].back()], wgt));
       }
     }
     as_before[x] = x > 0 && std::equal(owned[x].begin(), owned[x].end(), owned[x - 1].begin(), owned[x - 1].end(),
@@ -334,7 +357,7 @@ void level_plan(ExtendPlan& plan, const std::vector<Tile>& tiles, const std::vec
     }
     ordered = std::max(ordered, last_span);
   }
-  const bool reorder = ordered * 104 < now * 100;
+  const bool reorder = ordered * (100 + cm.reorder_percent) < now * 100;
   const int64_t best = reorder ? ordered : now;
 
   // the lowest level that holds everything (each cut adds an item's own cost)
@@ -342,27 +365,31 @@ void level_plan(ExtendPlan& plan, const std::vector<Tile>& tiles, const std::vec
   std::vector<int32_t> n_of(tiles.size(), 1);
   const int64_t base = (total + slots - 1) / slots;
   bool cut = false;
-  if ((base + kMergeCost) * 103 < best * 100 && best - base - kMergeCost >= kMinCutGain) {
+  if ((base + cm.merge) * 103 < best * 100 && best - base - cm.merge >= cm.min_cut_gain) {
     int64_t level = 0;
     for (int64_t k = 1; k <= 6 && !cut; ++k) {
-      level = base + k * (base / 100 + kItemCost / 4);
-      cut = level_queues(tiles, owned, as_before, wgt, R, level, pieces);
+      level = base + k * (base / 100 + cm.item / 4);
+      cut = level_queues(cm, tiles, owned, as_before, wgt, R, level, pieces);
     }
     if (cut) {
       std::fill(n_of.begin(), n_of.end(), 0);
       for (const auto& q : pieces)
         for (const Piece& p : q) ++n_of[p.tile];
-      int64_t n_parts = 0;
+      int64_t n_parts = 0, alone = 0;  // alone: work that loses the K/V which a bundle's tiles share
       size_t n_cut = 0;
-      for (const int32_t n : n_of) {
-        n_parts += n > 1 ? n : 0;
-        n_cut += n > 1 ? 1 : 0;
-      }
-      const int64_t then = level + kMergeCost + kMergePartCost * n_parts;
+      for (const Bd& bd : bundles)
+        for (int32_t i = bd.t0; i < bd.t0 + bd.n; ++i) {
+          if (n_of[i] < 2) continue;
+          n_parts += n_of[i];
+          n_cut += 1;
+          alone += tile_cost(cm, tiles[i], wgt) * (bd.n - 1) / bd.n;
+        }
+      const int64_t unshared = shared ? 0 : level * alone / total;
+      const int64_t then = level + unshared + cm.merge + cm.merge_part * n_parts;
       const int64_t slot_bytes = int64_t(plan.part_rows) * (head_dim * 4 + 8);
       const int64_t total_bytes =
           static_cast<int64_t>(plan_meta_bytes(plan.seqs.size(), launch_count(pieces), n_cut)) + n_parts * slot_bytes;
-      cut = then * 103 < best * 100 && best - then >= kMinCutGain && total_bytes <= kLevelTotalBytes;
+      cut = then * 103 < best * 100 && best - then >= cm.min_cut_gain && total_bytes <= cm.max_bytes;
     }
   }
   if (!cut && !reorder) return;
@@ -416,7 +443,8 @@ ExtendPlan build_extend_plan(const int32_t* prefix_lens, const int32_t* suffix_l
                              int32_t num_seqs, int32_t num_kv_heads, int32_t gqa_group,
                              int32_t head_dim, int32_t block_m, int32_t wgs_per_cu,
                              int32_t num_cus, int32_t num_xcds, const Tuning& tuning,
-                             const int32_t* cu_rows, const int32_t* bt_rows, int32_t maps) {
+                             const int32_t* cu_rows, const int32_t* bt_rows, int32_t maps,
+                             int64_t kv_bytes) {
   ExtendPlan plan;
   plan.part_rows = block_m * maps;
   plan.part_f32 = maps > 1;
@@ -444,7 +472,7 @@ ExtendPlan build_extend_plan(const int32_t* prefix_lens, const int32_t* suffix_l
         const int32_t kv_len = static_cast<int32_t>(prefix_lens[b] + t_last + 1);
         const int32_t n_kt = (kv_len + BLOCK_N - 1) / BLOCK_N;
         tiles.push_back(Tile{b, h, static_cast<int32_t>(r0), nr, kv_len, n_kt,
-                             std::min(n_kt, prefix_lens[b] / BLOCK_N)});
+                             std::min(n_kt, prefix_lens[b] / BLOCK_N), maps > 1 ? 100 : row_rate(nr)});
         total_kt += n_kt;
       }
     }
@@ -597,7 +625,8 @@ ExtendPlan build_extend_plan(const int32_t* prefix_lens, const int32_t* suffix_l
   }
   plan.whole_meta_bytes = plan_meta_bytes(plan.seqs.size(), launch_count(queues), plan.groups.size());
   if (tuning.kv_chunk_tiles == 0 && tuning.target_wgs == 0 && !dealt)
-    level_plan(plan, tiles, tile_bundles, std::max(1, tuning.suffix_weight), R, head_dim, queues);
+    level_plan(maps > 1 ? kDiffCosts : kExtendCosts, plan, tiles, tile_bundles, std::max(1, tuning.suffix_weight), R,
+               head_dim, maps, kv_bytes <= kSharedKvBytes, queues);
   size_t max_len = 0;
   for (auto& qv : queues) max_len = std::max(max_len, qv.size());
   const WorkItem idle{-1, 0, 0, 0, 0, -1, 0, 0};

@@ -14,8 +14,8 @@ namespace cw {
 // Plans of at most kMaxLevelTiles query tiles may be levelled (tiles cut into key
 // ranges so that all workgroups finish together; longer work lists are level
 // enough whole), if meta and partial slots then take at most kLevelTotalBytes (the
-// library's static scratch array) and the meta at most kLevelMetaBytes more than
-// the plan would have had otherwise.
+// library's static scratch array; with two maps three times that) and the meta at most
+// kLevelMetaBytes more than the plan would have had otherwise.
 constexpr int64_t kMaxLevelTiles = 4096;
 constexpr int64_t kLevelTotalBytes = int64_t(64) << 20;
 constexpr size_t kLevelMetaBytes = size_t(64) << 10;
@@ -63,13 +63,14 @@ struct ExtendPlan {
 // row is cu_rows[b] and its block-table row bt_rows[b] when given (a sub-batch
 // of a larger step), else the prefix sum of the suffix lengths and b.  With `maps` softmax
 // maps per query row a partial slot has maps * block_m rows of head_dim values, fp32 when
-// there are more than one (what the merge subtracts is not rounded before).
+// there are more than one (what the merge subtracts is not rounded before).  `kv_bytes`:
+// what the call's K/V takes, where that decides whether tiles are cut (else 0).
 ExtendPlan build_extend_plan(const int32_t* prefix_lens, const int32_t* suffix_lens,
                              int32_t num_seqs, int32_t num_kv_heads, int32_t gqa_group,
                              int32_t head_dim, int32_t block_m, int32_t wgs_per_cu,
                              int32_t num_cus, int32_t num_xcds, const Tuning& tuning,
                              const int32_t* cu_rows = nullptr, const int32_t* bt_rows = nullptr,
-                             int32_t maps = 1);
+                             int32_t maps = 1, int64_t kv_bytes = 0);
 
 // Bytes of a decode plan in compact form whose records start at byte `at`.
 inline size_t compact_bytes(size_t at, size_t n_seqs, size_t n_tails) {

@@ -124,6 +124,23 @@ def test_split_keys(tiles, dt, d):
         cwlib.set_tuning(0, 0)
 
 
+@pytest.mark.parametrize("d,page,dt", [(64, 16, "bf16"), (128, 64, "fp8")])
+def test_levelled_plan(d, page, dt):
+    """More query tiles than CUs, and far from a multiple: some are cut into key ranges. Another
+    plan than with whole tiles (a target of 256 workgroups), the same result within the bounds."""
+    print(f"\n[case] diff levelled {d} {dt}", flush=True)
+    w, dw, lam, weight = _inputs([1500, 1400, 900, 1600, 1300, 700, 1500], [700, 650, 640, 600, 690, 710, 500], 2, 4, d, page,
+                                 dt, seed=29)  # 286 tiles
+    got = _check(w, dw, lam, weight, f"diff levelled {d} {dt}")
+    cwlib.set_tuning(1, 256)
+    try:
+        whole = _run(dw, lam, weight)
+    finally:
+        cwlib.set_tuning(1, 0)
+    torch.cuda.synchronize()
+    assert not torch.equal(got, whole)
+
+
 @pytest.mark.parametrize("knob,value", [(4, 1), (6, 0), (7, 0)])
 def test_plan_paths_give_the_same_bits(knob, value):
     """Plans read from the staging slot, uploaded in full, or not in the kernel arguments."""
