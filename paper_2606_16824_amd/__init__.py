@@ -13,6 +13,10 @@ fallback: without the built library every call raises.
     kv_write_pages(k_new, v_new, k_pool, v_pool, block_table, prefix_lens,
                    suffix_lens, k_scale=None, v_scale=None, workspace=None)
 
+and, of include/cw_layer.h, what a layer does around its attention: build_step_tables
+(block table and slots from lengths on the GPU), qk_norm_rope (norm, rotation and page
+write) and diff_attention (differential attention over pools of paired heads).
+
 Page size and head dim are read from the pool shape [num_pages, Hkv, P, D];
 an fp8 pool is a uint8 (or float8_e4m3fn) tensor of e4m3fn codes.
 

@@ -3,7 +3,7 @@
 // A workgroup of eight waves owns 128 packed query rows (token x query pair of one key
 // pair): waves 0-3 compute the first map of 32 rows each, waves 4-7 the second map of
 // the same rows.  Both read the same value tile, twice as wide as a key, so per 32 keys a
-// wave runs D / 16 MFMAs of scores and D / 4 of values against 16 exponentials per lane.
+// wave runs D / 16 MFMAs of scores and D / 8 of values against 16 exponentials per lane.
 // At the end the second map's waves hand over lam O2 / l2 through LDS and the first map's
 // waves subtract, norm and store.  The difference is taken once per row, after both
 // softmaxes: taking it in the weights would need the row sums first.
