@@ -541,18 +541,16 @@ _TABLES_WITHOUT_WORKSPACE = 4096  # cw_step_tables_workspace_bytes is 0 up to he
 
 def _quick_tables(dev, num, t, prefix_lens, suffix_lens, free_pages, block_table, cu_rows, seq_ids, positions, slots, info):
     """Whether every check of build_step_tables passes (else they are made one at a time): the
-    call's own work takes 4 us on the GPU."""
-    i32, i64 = torch.int32, torch.int64
+    call's own work takes 3 us on the GPU."""
+    i32, i64, row = torch.int32, torch.int64, (1,)
     try:
-        for x, n in ((prefix_lens, num), (suffix_lens, num), (free_pages, -1), (cu_rows, num + 1), (seq_ids, t),
-                     (positions, t)):
-            if not (x.dtype is i32 and x.dim() == 1 and (x.shape[0] == n or n < 0) and x.get_device() == dev
-                    and x.is_contiguous()):
+        for x, n in ((prefix_lens, num), (suffix_lens, num), (cu_rows, num + 1), (seq_ids, t), (positions, t)):
+            if not (x.dtype is i32 and x.stride() == row and x.numel() == n and x.get_device() == dev):
                 return False
-        for x, n in ((slots, t), (info, 3)):
-            if not (x.dtype is i64 and x.dim() == 1 and x.shape[0] == n and x.get_device() == dev and x.is_contiguous()):
-                return False
-        return (block_table.dtype is i32 and block_table.dim() == 2 and block_table.shape[0] >= num
+        return (slots.dtype is i64 and slots.stride() == row and slots.numel() == t and slots.get_device() == dev
+                and info.dtype is i64 and info.stride() == row and info.numel() == 3 and info.get_device() == dev
+                and free_pages.dtype is i32 and free_pages.stride() == row and free_pages.get_device() == dev
+                and block_table.dtype is i32 and block_table.dim() == 2 and block_table.shape[0] >= num
                 and block_table.get_device() == dev and block_table.is_contiguous())
     except AttributeError:
         return False

@@ -12,9 +12,10 @@
 // tokens and pages, each thread searching its sequence in LDS.  A thread reads the lengths
 // of its (at most four) sequences at once.  Longer lists are summed by one workgroup into
 // the workspace first.  All arithmetic on lengths is in 32 bits, clipped, with shifts for the
-// page size: in 64 bits with divisions the largest steps were bound by it.  GPU time of 8
-// sequences 3.6 us, of 64 with 8.9k tokens 4.7 us, of 3500 with 304k tokens 12.0 us (20.7 us
-// in 64 bits).
+// page size: in 64 bits with divisions the largest steps were bound by it.  A page's and a
+// token's loads go out together, and a workgroup of its own sums `info`.  Time in a graph of 8
+// sequences 2.8 us (3.8 with `info` by the last workgroup and pages before tokens), of 200
+// with 25k tokens 4.2, of 3500 with 304k tokens 9.7 us (20.7 in 64 bits).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -28,6 +29,9 @@ namespace {
 constexpr int kScanThreads = 1024;
 constexpr int kPer = 4;  // sequences per thread of the one-launch form
 constexpr int kMaxBlocks = 1024;
+// Of 1024 threads, which all sum the lengths (2.5 us of vector work at four waves per SIMD): one
+// to a CU, and info's. 3500 sequences with 304k tokens: 298 workgroups 11.0 us, 255 9.7.
+constexpr int kMaxWideBlocks = 255;
 
 // Sums of lengths are clipped at INT32_MAX (rows and entries past it exist nowhere); both
 // terms are at most that, so their sum fits uint32.
@@ -177,51 +181,61 @@ __device__ __forceinline__ int last_at_most(const T* first, int n, int32_t x) {
   return lo;
 }
 
-// This workgroup's share of the tokens, of the new pages and of cu_rows; `lens`: the
-// prefix lengths as given.
-__device__ __forceinline__ void fill(const StepTablesParams& p, const int32_t* rows, const int32_t* pages, const int32_t* lens) {
+// The share of `me` among `of` workgroups of the tokens, of the new pages and of cu_rows;
+// `lens`: the prefix lengths as given.
+__device__ __forceinline__ void fill(const StepTablesParams& p, const int32_t* rows, const int32_t* pages,
+                                     const int32_t* lens, int me, int of) {
   const int n = p.num_seqs;
   const int total_rows = rows[n], total_pages = pages[n];
-  const int64_t stride = int64_t(gridDim.x) * blockDim.x, first = int64_t(blockIdx.x) * blockDim.x + threadIdx.x;
+  const int64_t stride = int64_t(of) * blockDim.x, first = int64_t(me) * blockDim.x + threadIdx.x;
   auto free_page = [&](uint32_t f) -> int32_t { return f < uint32_t(p.num_free) ? p.free_pages[f] : -1; };
   auto held_of = [&](uint32_t lp) -> int32_t { return min(pages_of(p, lp), p.bt_stride); };
-  for (int64_t f = first; f < total_pages; f += stride) {
-    const int b = last_at_most(pages, n, static_cast<int32_t>(f));
-    const int col = held_of(max(lens[b], 0)) + static_cast<int32_t>(f - pages[b]);
-    p.block_table[int64_t(b) * p.bt_stride + col] = free_page(static_cast<uint32_t>(f));
-  }
-  for (int64_t t = first; t < p.max_tokens; t += stride) {
-    int32_t seq = -1, pos = -1;
-    int64_t slot = -1;
-    if (t < total_rows) {
-      seq = last_at_most(rows, n, static_cast<int32_t>(t));
+  const int64_t last = max(int64_t(total_pages), max(int64_t(p.max_tokens), int64_t(n) + 1));
+  for (int64_t i = first; i < last; i += stride) {
+    // new page i and token i: their loads go out before either is stored
+    const bool page = i < total_pages, token = i < p.max_tokens;
+    int32_t new_page = -1;
+    int64_t entry = 0;
+    if (page) {
+      const int b = last_at_most(pages, n, static_cast<int32_t>(i));
+      entry = int64_t(b) * p.bt_stride + held_of(max(lens[b], 0)) + (static_cast<int32_t>(i) - pages[b]);
+      new_page = free_page(static_cast<uint32_t>(i));
+    }
+    int32_t seq = -1, pos = -1, pg = -1, in_page = 0;
+    if (token && i < total_rows) {
+      seq = last_at_most(rows, n, static_cast<int32_t>(i));
       const uint32_t lp = max(lens[seq], 0);
       const int32_t held = held_of(lp);
-      const uint32_t at = lp + static_cast<uint32_t>(t - rows[seq]);
+      const uint32_t at = lp + static_cast<uint32_t>(i - rows[seq]);
       const int32_t col = static_cast<int32_t>(at >> p.page_shift);
       pos = static_cast<int32_t>(min(at, uint32_t(INT32_MAX)));
-      if (col < p.bt_stride && p.slots != nullptr) {
+      in_page = static_cast<int32_t>(at & ((1u << p.page_shift) - 1u));
+      if (col < p.bt_stride && p.slots != nullptr)
         // a page of this step is read from the free list: another workgroup writes the table
-        const int32_t pg = col < held ? p.block_table[int64_t(seq) * p.bt_stride + col]
-                                      : free_page(static_cast<uint32_t>(pages[seq]) + static_cast<uint32_t>(col - held));
-        if (pg >= 0) slot = (int64_t(pg) << p.page_shift) + (at & ((1u << p.page_shift) - 1u));
-      }
+        pg = col < held ? p.block_table[int64_t(seq) * p.bt_stride + col]
+                        : free_page(static_cast<uint32_t>(pages[seq]) + static_cast<uint32_t>(col - held));
     }
-    if (p.seq_ids != nullptr) p.seq_ids[t] = seq;
-    if (p.positions != nullptr) p.positions[t] = pos;
-    if (p.slots != nullptr) p.slots[t] = slot;
+    if (i <= n && p.cu_rows != nullptr) p.cu_rows[i] = rows[i];
+    if (page) p.block_table[entry] = new_page;
+    if (token) {
+      if (p.seq_ids != nullptr) p.seq_ids[i] = seq;
+      if (p.positions != nullptr) p.positions[i] = pos;
+      if (p.slots != nullptr) p.slots[i] = pg >= 0 ? (int64_t(pg) << p.page_shift) + in_page : -1;
+    }
   }
-  if (p.cu_rows != nullptr)
-    for (int64_t b = first; b <= n; b += stride) p.cu_rows[b] = rows[b];
 }
 
 template <int N>
 __global__ __launch_bounds__(N) void step_tables_kernel(StepTablesParams p) {
   __shared__ int32_t rows[N * kPer + 1], pages[N * kPer + 1], lens[N * kPer];
+  const int fills = static_cast<int>(gridDim.x) - (p.info != nullptr ? 1 : 0);
+  if (static_cast<int>(blockIdx.x) == fills) {  // the last workgroup, besides the others
+    put_info<N>(p);
+    return;
+  }
   sum_lengths<N, kPer>(p, rows, pages, lens);
   __syncthreads();
-  fill(p, rows, pages, lens);
-  if (blockIdx.x == gridDim.x - 1 && p.info != nullptr) put_info<N>(p);
+  fill(p, rows, pages, lens, static_cast<int>(blockIdx.x), fills);
 }
 
 __global__ __launch_bounds__(kScanThreads) void step_tables_sum_kernel(StepTablesParams p) {
@@ -230,7 +244,7 @@ __global__ __launch_bounds__(kScanThreads) void step_tables_sum_kernel(StepTable
 }
 
 __global__ __launch_bounds__(256) void step_tables_fill_kernel(StepTablesParams p) {
-  fill(p, p.sums, p.sums + p.num_seqs + 1, p.prefix_lens);
+  fill(p, p.sums, p.sums + p.num_seqs + 1, p.prefix_lens, static_cast<int>(blockIdx.x), static_cast<int>(gridDim.x));
 }
 
 }  // namespace
@@ -238,22 +252,23 @@ __global__ __launch_bounds__(256) void step_tables_fill_kernel(StepTablesParams 
 hipError_t launch_step_tables(const StepTablesParams& p, hipStream_t stream) {
   // a token (or entry of cu_rows) per thread; a step has at most as many new pages as new tokens
   const int64_t work = std::max<int64_t>(p.max_tokens, p.num_seqs + 1);
-  auto grid = [&](int64_t threads) {
-    return dim3(static_cast<unsigned>(std::min<int64_t>((work + threads - 1) / threads, kMaxBlocks)));
+  auto grid = [&](int64_t threads, int more) {
+    return dim3(static_cast<unsigned>(std::min<int64_t>((work + threads - 1) / threads, threads == kScanThreads ? kMaxWideBlocks : kMaxBlocks) + more));
   };
+  const int info = p.info != nullptr ? 1 : 0;  // a workgroup of its own in the one-launch form
   static_assert(1024 * kPer == kStepTablesLdsSeqs, "the largest one-launch form");
   if (p.num_seqs <= 64 * kPer) {
-    hipLaunchKernelGGL((step_tables_kernel<64>), grid(64), dim3(64), 0, stream, p);
+    hipLaunchKernelGGL((step_tables_kernel<64>), grid(64, info), dim3(64), 0, stream, p);
     return hipGetLastError();
   }
   if (p.num_seqs <= kStepTablesLdsSeqs) {
-    hipLaunchKernelGGL((step_tables_kernel<1024>), grid(1024), dim3(1024), 0, stream, p);
+    hipLaunchKernelGGL((step_tables_kernel<1024>), grid(kScanThreads, info), dim3(kScanThreads), 0, stream, p);
     return hipGetLastError();
   }
   hipLaunchKernelGGL(step_tables_sum_kernel, dim3(1), dim3(kScanThreads), 0, stream, p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(step_tables_fill_kernel, grid(256), dim3(256), 0, stream, p);
+  hipLaunchKernelGGL(step_tables_fill_kernel, grid(256, 0), dim3(256), 0, stream, p);
   return hipGetLastError();
 }
 
