@@ -26,9 +26,9 @@
 // 128 KB of LDS, one workgroup per CU.
 //
 // Bound by the matrix cores: 4096 new tokens on 32768 cached ones, 8 key pairs of 4 query
-// pairs at D = 128, take 6.05 ms, 1159 TFLOP/s (a plain bf16 product of 8192^3 reaches 1214);
-// at D = 64 (half the matrix work per exponential) 1068 TFLOP/s; over fp8 pools, whose
-// rows are widened on the way, 1026 and 933.  (Cards differ by up to 10%.)
+// pairs at D = 128, take 5.9-6.2 ms, 1139-1186 TFLOP/s (a plain bf16 product of 8192^3
+// reaches 1214); at D = 64 (half the matrix work per exponential) 1034-1070 TFLOP/s; over
+// fp8 pools, whose rows are widened on the way, 1000-1050 and 905-933.
 #include <hip/hip_runtime.h>
 
 #include "../cw_internal.h"
@@ -45,6 +45,9 @@ typedef __attribute__((address_space(4))) const int32_t const_i32;
 typedef __attribute__((address_space(4))) const float const_f32;
 
 constexpr int kWaves = 8, kThreads = kWaves * 64;
+// What the compiler may move across the point between a fragment's read and a product: vector,
+// scalar and transcendental operations (the weights' exponentials run beside the products).
+constexpr int kMayCross = 0x2 | 0x4 | 0x400;
 constexpr int kAhead = 32;  // keys by which key tiles lie behind value tiles
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc_at(const void* base) {
@@ -116,6 +119,11 @@ struct Geo {
   static constexpr int KT = D / 16;                  // k-steps of K Q^T
   static constexpr int DB = D / 32;                  // 32-row blocks of O^T per value half
   static constexpr int VB = 2 * DB;
+  // Fragments read ahead of their products.  At D = 128, left to the compiler, each product
+  // waited for its own read (matrix cores busy 53% of the cycles): 4096 tokens on 32768 keys, 4
+  // key pairs, 3.05-3.12 ms, with these 2.95-3.03, over fp8 pages 3.42-3.49 and 3.34-3.43.  At D =
+  // 64 the compiler's own order is 1-2% faster than any with reads ahead.
+  static constexpr int K_AHEAD = D == 64 ? 0 : FP8 ? 1 : 2, V_AHEAD = D == 64 ? 0 : 2;
   static constexpr int PRB = FP8 ? D : RB;           // bytes per pool row
   static constexpr int B8 = D / 8;                   // fp8 bytes each lane stages per matrix
   static_assert(NI * RPI == 8, "each wave stages 8 rows of a tile");
@@ -337,10 +345,15 @@ void diff_extend_kernel(DiffParams dp, PlanArg<AP> ap) {
 
   // scores of the 32 keys in rows 32 blk on of key tile kt
   auto scores = [&](const uint8_t* kt, int blk, f32x16& s) __attribute__((always_inline)) {
+    u32x4 kf[T::KT];
+    auto read = [&](int kk) { kf[kk] = *reinterpret_cast<const u32x4*>(kt + k_addr[kk] + blk * 32 * T::RB); };
+#pragma unroll
+    for (int kk = 0; kk < T::K_AHEAD && kk < T::KT; ++kk) read(kk);
 #pragma unroll
     for (int kk = 0; kk < T::KT; ++kk) {
-      const u32x4 kf = *reinterpret_cast<const u32x4*>(kt + k_addr[kk] + blk * 32 * T::RB);
-      s = mfma16<FP8>(kf, qf[kk], kk > 0 ? s : f32x16{});
+      if (kk + T::K_AHEAD < T::KT) read(kk + T::K_AHEAD);
+      if constexpr (D == 128) __builtin_amdgcn_sched_barrier(kMayCross);
+      s = mfma16<FP8>(kf[kk], qf[kk], kk > 0 ? s : f32x16{});
     }
   };
   // causal mask of the block of keys from k0 on: element i holds key k0 + 16 (i / 8) + 8 h + i % 8
@@ -392,18 +405,23 @@ void diff_extend_kernel(DiffParams dp, PlanArg<AP> ap) {
   };
   // O^T += V^T P^T over the 32 keys in rows 32 blk on of value tile vt
   auto accumulate = [&](const uint8_t* vt, int blk, const u32x4(&pf)[2]) __attribute__((always_inline)) {
+    u32x4 vf[2 * T::VB];
+    auto read = [&](int i) __attribute__((always_inline)) {
+      const int u = i / T::VB, b = i % T::VB;
+      i16x4 part[2];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
+      for (int e4 = 0; e4 < 2; ++e4)
+        part[e4] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (lds_i16x4*)(vt + (b / T::DB) * T::TILE + v_addr[b % T::DB] + (32 * blk + 16 * u + 4 * e4) * T::RB));
+      vf[i] = __builtin_bit_cast(u32x4, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
+    };
 #pragma unroll
-      for (int b = 0; b < T::VB; ++b) {
-        i16x4 part[2];
+    for (int i = 0; i < T::V_AHEAD; ++i) read(i);
 #pragma unroll
-        for (int e4 = 0; e4 < 2; ++e4)
-          part[e4] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-              (lds_i16x4*)(vt + (b / T::DB) * T::TILE + v_addr[b % T::DB] + (32 * blk + 16 * u + 4 * e4) * T::RB));
-        const u32x4 vf = __builtin_bit_cast(u32x4, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
-        o[b] = mfma16<FP8>(vf, pf[u], o[b]);
-      }
+    for (int i = 0; i < 2 * T::VB; ++i) {
+      if (i + T::V_AHEAD < 2 * T::VB) read(i + T::V_AHEAD);
+      if constexpr (D == 128) __builtin_amdgcn_sched_barrier(kMayCross);
+      o[i % T::VB] = mfma16<FP8>(vf[i], pf[i / T::VB], o[i % T::VB]);
     }
   };
   // One block of 32 keys: the next block's scores (rows 32 blk on of key tile kt, keys from
