@@ -431,6 +431,10 @@ void diff_extend_kernel(DiffParams dp, PlanArg<AP> ap) {
     u32x4 pf[2];
     float lsum;
     scores(kt, blk, s);
+    // At D = 64 a wave that forms weights goes before the one on its SIMD that feeds the matrix
+    // cores: 4096 tokens on 32768 keys 1680 -> 1659 us, over fp8 pages 1915 -> 1861 (D = 128:
+    // between 1% less and 1% more).
+    if constexpr (D == 64) __builtin_amdgcn_s_setprio(1);
     weights(x, pf, lsum);
     if (__any(!(lsum <= kSumLimit))) {
       const float mx = fmaxf(block_max(x) - kHeadroom, m_run);
@@ -442,6 +446,7 @@ void diff_extend_kernel(DiffParams dp, PlanArg<AP> ap) {
       weights(x, pf, lsum);
     }
     l_run += lsum;
+    if constexpr (D == 64) __builtin_amdgcn_s_setprio(0);
     if (edge) mask(k_next, s);
     accumulate(vt, blk, pf);
   };
