@@ -685,15 +685,18 @@ std::shared_ptr<const StepPlan> step_plan(const int32_t* lp, const int32_t* ls, 
                                           int32_t num_kv_heads, int32_t gqa_group, int32_t head_dim,
                                           int32_t page_size, cw_kv_dtype_t kv_dtype) {
   thread_local LastPlan<StepPlan> last;
-  const PlanKinds kinds{
-      [&](const PlanEnv& env, const int32_t* lp_e, const int32_t* ls_e, int32_t n, const int32_t* cu, const int32_t* bt) {
-        return make_plan(env, lp_e, ls_e, n, num_kv_heads, gqa_group, head_dim, cu, bt);
-      },
-      [&](const PlanEnv& env, const int32_t* lp_d, int32_t n, size_t meta_at, const int32_t* cu, const int32_t* bt) {
-        return make_decode_plan(env, lp_d, n, num_kv_heads, gqa_group, head_dim, page_size, kv_dtype, meta_at, cu, bt);
-      }};
-  return last.get(lp, ls, num_seqs, {num_kv_heads, gqa_group, head_dim, page_size, int32_t(kv_dtype)},
-                  [&](const PlanEnv& env) { return make_step_plan(env, lp, ls, num_seqs, kinds); }, step_kept_bytes);
+  auto make = [&](const PlanEnv& e) {  // (the kinds are built with a plan only: they allocate)
+    const PlanKinds kinds{
+        [&](const PlanEnv& env, const int32_t* lp_e, const int32_t* ls_e, int32_t n, const int32_t* cu, const int32_t* bt) {
+          return make_plan(env, lp_e, ls_e, n, num_kv_heads, gqa_group, head_dim, cu, bt);
+        },
+        [&](const PlanEnv& env, const int32_t* lp_d, int32_t n, size_t meta_at, const int32_t* cu, const int32_t* bt) {
+          return make_decode_plan(env, lp_d, n, num_kv_heads, gqa_group, head_dim, page_size, kv_dtype, meta_at, cu, bt);
+        }};
+    return make_step_plan(e, lp, ls, num_seqs, kinds);
+  };
+  return last.get(lp, ls, num_seqs, {num_kv_heads, gqa_group, head_dim, page_size, int32_t(kv_dtype)}, make,
+                  step_kept_bytes);
 }
 
 // The plan of a differential attention call: like a step's, of its key pairs, with the
@@ -702,21 +705,23 @@ std::shared_ptr<const StepPlan> diff_plan(const int32_t* lp, const int32_t* ls, 
                                           int32_t gqa_group, int32_t head_dim, int32_t page_size,
                                           cw_kv_dtype_t kv_dtype) {
   thread_local LastPlan<StepPlan> last;
-  const bool fp8 = kv_dtype == CW_KV_FP8_E4M3FN;
-  const PlanKinds kinds{
-      [&](const PlanEnv& env, const int32_t* lp_e, const int32_t* ls_e, int32_t n, const int32_t* cu, const int32_t* bt) {
-        int64_t kv_bytes = 0;  // K and V of both heads of every pair
-        for (int32_t b = 0; b < n; ++b)
-          kv_bytes += (int64_t(lp_e[b]) * (fp8 ? 1 : 2) + int64_t(ls_e[b]) * 2) * 4 * head_dim * num_pairs;
-        return build_extend_plan(lp_e, ls_e, n, num_pairs, gqa_group, 2 * head_dim, DIFF_BLOCK_M, 1, env.cus, env.xcds,
-                                 env.tuning, cu, bt, 2, kv_bytes);
-      },
-      [&](const PlanEnv& env, const int32_t* lp_d, int32_t n, size_t meta_at, const int32_t* cu, const int32_t* bt) {
-        return build_decode_plan(lp_d, n, num_pairs, gqa_group, 2 * head_dim, page_size, diff_decode_keys_per_tile(),
-                                 diff_decode_waves_per_cu(head_dim, fp8), env.cus, env.tuning, meta_at, cu, bt, 2);
-      }};
-  return last.get(lp, ls, num_seqs, {num_pairs, gqa_group, head_dim, page_size, int32_t(kv_dtype)},
-                  [&](const PlanEnv& env) { return make_step_plan(env, lp, ls, num_seqs, kinds); }, step_kept_bytes);
+  auto make = [&](const PlanEnv& e) {
+    const bool fp8 = kv_dtype == CW_KV_FP8_E4M3FN;
+    const PlanKinds kinds{
+        [&](const PlanEnv& env, const int32_t* lp_e, const int32_t* ls_e, int32_t n, const int32_t* cu, const int32_t* bt) {
+          int64_t kv_bytes = 0;  // K and V of both heads of every pair
+          for (int32_t b = 0; b < n; ++b)
+            kv_bytes += (int64_t(lp_e[b]) * (fp8 ? 1 : 2) + int64_t(ls_e[b]) * 2) * 4 * head_dim * num_pairs;
+          return build_extend_plan(lp_e, ls_e, n, num_pairs, gqa_group, 2 * head_dim, DIFF_BLOCK_M, 1, env.cus, env.xcds,
+                                   env.tuning, cu, bt, 2, kv_bytes);
+        },
+        [&](const PlanEnv& env, const int32_t* lp_d, int32_t n, size_t meta_at, const int32_t* cu, const int32_t* bt) {
+          return build_decode_plan(lp_d, n, num_pairs, gqa_group, 2 * head_dim, page_size, diff_decode_keys_per_tile(),
+                                   diff_decode_waves_per_cu(head_dim, fp8), env.cus, env.tuning, meta_at, cu, bt, 2);
+        }};
+    return make_step_plan(e, lp, ls, num_seqs, kinds);
+  };
+  return last.get(lp, ls, num_seqs, {num_pairs, gqa_group, head_dim, page_size, int32_t(kv_dtype)}, make, step_kept_bytes);
 }
 
 // Kernel arguments of a plan whose meta is read at `meta` and whose partials
