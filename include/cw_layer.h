@@ -45,8 +45,8 @@ extern "C" {
  * prefix_lens, suffix_lens: device int32 [num_seqs]; free_pages: device int32
  * [num_free], distinct page ids; block_table: device int32 [num_seqs, bt_stride];
  * cu_rows [num_seqs + 1], seq_ids, positions [max_tokens] int32, slots [max_tokens] and
- * info [3] int64, device, each may be NULL.  page_size 16 or 64.  Outputs may overlap
- * neither inputs nor each other (CW_ERR_ALIAS).  Workspace:
+ * info [3] int64, device, each may be NULL.  page_size 16 or 64, num_seqs up to 2^30.
+ * Outputs may overlap neither inputs nor each other (CW_ERR_ALIAS).  Workspace:
  * cw_step_tables_workspace_bytes(num_seqs) bytes, 0 up to 4096 sequences (then it may be
  * NULL).  Needs no cw_init, also under capture. */
 size_t cw_step_tables_workspace_bytes(int32_t num_seqs);

@@ -1385,6 +1385,8 @@ cw_status_t cw_build_step_tables(const int32_t* prefix_lens, const int32_t* suff
     if (num_seqs < 0 || num_free < 0 || max_tokens < 0)
       return fail(CW_ERR_BAD_LENS, "negative count (num_seqs = %d, num_free = %d, max_tokens = %d)", num_seqs, num_free,
                   max_tokens);
+    if (num_seqs > kStepTablesMaxSeqs)
+      return fail(CW_ERR_BAD_LENS, "num_seqs = %d (supported: up to %d)", num_seqs, kStepTablesMaxSeqs);
     if (num_seqs > 0 && bt_stride < 1) return fail(CW_ERR_BAD_LENS, "bt_stride = %d must be >= 1", bt_stride);
     if (num_seqs > 0 && (!prefix_lens || !suffix_lens || !block_table))
       return fail(CW_ERR_NULL, "prefix_lens, suffix_lens and block_table are required");

@@ -173,6 +173,7 @@ struct SwapParams {
 
 // Tables of a serving step, from lengths on the device (step_tables.hip).
 constexpr int kStepTablesLdsSeqs = 4096;  // up to here one launch, every workgroup summing the lengths itself
+constexpr int kStepTablesMaxSeqs = 1 << 30;   // the kernels step through sequences in 32-bit indexes
 struct StepTablesParams {
   const int32_t* prefix_lens;  // [num_seqs], device
   const int32_t* suffix_lens;
