@@ -116,8 +116,9 @@ cw_status_t cw_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int6
  * Supported: head_dim 64 or 128, page_size 16 or 64, gqa_group 1..16, num_kv_pairs
  * 1..512; out_scale finite, norm_eps finite and >= 0.  Sequences with one new token run on
  * the HBM-streaming kernel, the others on the matrix-core kernel, which over fp8 pools
- * computes in fp16: |code * scale| and every q, k_new and v_new value of such a call must
- * lie below 65504 (and is held to 2^-25 where it lies below 2^-14).  The streaming kernel has
+ * takes q, k_new, v_new and the cached values (code * scale) in fp16: of such a call their
+ * magnitudes must lie below 65504 (and are held to 2^-25 where they lie below 2^-14).  Key
+ * scales are applied to the scores in fp32 by both.  The streaming kernel has
  * no such limit, but takes the V scales of the pages that a sequence's weight lies on to be
  * within 2^20 of each other.  A scale may be 0 (a page of zeros).  With a norm, mean(x_h^2)
  * must be an fp32 number: values below about 2^59.  A NaN or infinity in a new token's value may reach the rows of earlier

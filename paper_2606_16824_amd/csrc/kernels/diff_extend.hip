@@ -8,8 +8,13 @@
 // waves subtract, norm and store.  The difference is taken once per row, after both
 // softmaxes: taking it in the weights would need the row sums first.
 //
-// S^T = K Q^T and O^T += V^T P^T with v_mfma_f32_32x32x16 (bf16; fp16 over fp8 pools,
-// whose rows are widened into LDS with their page's scale, as the extend kernel does).
+// S^T = K Q^T and O^T += V^T P^T with v_mfma_f32_32x32x16 (bf16; fp16 over fp8 pools).  fp8
+// rows are widened into LDS, values with their page's scale (2^-10 of a value in all), key
+// codes as they are, which fp16 holds exactly: their page's scale multiplies the scores in
+// fp32 with the softmax scale, so that no error but fp32's grows with the scores (the scale
+// rounded to fp16 and applied to the keys moved a page's weights by 2^-11 of its scores, 3% at
+// scores of 60).  A 16-key group has one page and so one scale, a scalar; where the prefix ends
+// inside a group its scores are scaled one by one.
 // Softmax scale and running max enter the exponent in fp32, exp2(s c - m); the weights
 // are rounded to the operand type (bf16: 2^-8 relative at most) and their sum is taken
 // after that, so numerator and denominator agree.  For bf16 pools that rounding is the
@@ -50,6 +55,10 @@ constexpr int kWaves = 8, kThreads = kWaves * 64;
 constexpr int kMayCross = 0x2 | 0x4 | 0x400;
 constexpr int kAhead = 32;  // keys by which key tiles lie behind value tiles
 
+// What is known of a block of keys whose scores are taken: all in the cached prefix, all among the
+// new tokens and visible to every row, or neither.
+enum class Keys { kPrefix, kNew, kMasked };
+
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc_at(const void* base) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, -1, 0x00020000);
 }
@@ -77,9 +86,17 @@ __device__ __forceinline__ uint32_t fp8x2_f16x2(uint32_t w, PageScale sc) {
   const f16x2 v = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(static_cast<int>(w), sc.p2, HI);
   return __builtin_bit_cast(uint32_t, v * sc.fm);
 }
+// Eight codes times their page's scale (values), or as they are (keys: exact).
 __device__ __forceinline__ u32x4 fp8x8_f16x8(uint32_t lo, uint32_t hi, PageScale sc) {
   return u32x4{fp8x2_f16x2<false>(lo, sc), fp8x2_f16x2<true>(lo, sc), fp8x2_f16x2<false>(hi, sc),
                fp8x2_f16x2<true>(hi, sc)};
+}
+__device__ __forceinline__ u32x4 fp8x8_f16x8(uint32_t lo, uint32_t hi) {
+  auto two = [](f16x2 v) { return __builtin_bit_cast(uint32_t, v); };
+  return u32x4{two(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(static_cast<int>(lo), 1.f, false)),
+               two(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(static_cast<int>(lo), 1.f, true)),
+               two(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(static_cast<int>(hi), 1.f, false)),
+               two(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(static_cast<int>(hi), 1.f, true))};
 }
 __device__ __forceinline__ u32x4 bf16x8_f16x8(u32x4 x) {
   u32x4 r;
@@ -126,6 +143,7 @@ struct Geo {
   static constexpr int K_AHEAD = D == 64 ? 0 : FP8 ? 1 : 2, V_AHEAD = D == 64 ? 0 : 2;
   static constexpr int PRB = FP8 ? D : RB;           // bytes per pool row
   static constexpr int B8 = D / 8;                   // fp8 bytes each lane stages per matrix
+  static constexpr int KS = BLOCK_N / (P < 32 ? P : 32);  // fp8: key scales kept per tile, one per page and block
   static_assert(NI * RPI == 8, "each wave stages 8 rows of a tile");
 };
 
@@ -211,17 +229,12 @@ void diff_extend_kernel(DiffParams dp, PlanArg<AP> ap) {
   }
   const uint32_t page_bytes = uint32_t(P) * T::PRB;  // one (page, head) block
   // fp8 rows.  D = 64: lane l stages 8 bytes of row 8 w + l / 8.  D = 128: load u of lane
-  // l fetches what belongs at position l % 16 of row 8 w + 4 u + l / 16.
-  uint32_t k8_off[2], v8_off[2];
-  int r8[2];
-#pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    const int R = D == 128 ? wrow0 + 4 * u + (lane >> 4) : wrow0 + (lane >> 3);
-    const int pos = D == 128 ? lane & 15 : lane & 7;
-    r8[u] = R;
-    k8_off[u] = uint32_t(((R + kAhead) % P) * D + 8 * (pos ^ k_swz<D>(R)));
-    v8_off[u] = uint32_t((R % P) * D + 8 * (pos ^ v_swz<D>(R)));
-  }
+  // l fetches what belongs at position l % 16 of row 8 w + 4 u + l / 16 (four rows on, a key's
+  // swizzle differs in the bit of 8, a value's not at all).
+  const int r8 = D == 128 ? wrow0 + (lane >> 4) : wrow0 + (lane >> 3);
+  const int pos8 = D == 128 ? lane & 15 : lane & 7;
+  const uint32_t k8_off = uint32_t(((r8 + kAhead) % P) * D + 8 * (pos8 ^ k_swz<D>(r8)));
+  const uint32_t v8_off = uint32_t((r8 % P) * D + 8 * (pos8 ^ v_swz<D>(r8)));
 
   const_i32* bt_s = (const_i32*)bt;
   const_f32* ks_s = (const_f32*)p.k_scale;
@@ -263,41 +276,42 @@ void diff_extend_kernel(DiffParams dp, PlanArg<AP> ap) {
   const uint8_t* k_pool_pair = k_pool + size_t(2 * pair) * page_bytes;
   const uint8_t* v_pool_pair = v_pool + size_t(2 * pair) * page_bytes;
   const size_t page_stride = size_t(hkv) * page_bytes;
-  // fp8 pool rows of both matrices into registers, with their page's scales (`in_prefix`: the
+  // fp8 pool rows of both matrices into registers, values with their page's scales (`in_prefix`: the
   // tile lies wholly in the cached prefix, so every row check passes)
   struct Rows8 {
     u32x4 x[2];
     float s[2];
   };
-  auto load8 = [&](int j0, int pg, const uint8_t* pool_pair, const_f32* scales, const uint32_t(&off)[2],
-                   Rows8& rw, bool in_prefix) __attribute__((always_inline)) {
+  auto load8 = [&](int j0, int pg, const uint8_t* pool_pair, uint32_t off,
+                   Rows8& rw, bool in_prefix, bool keys) __attribute__((always_inline)) {
     if (!in_prefix && j0 + wrow0 >= lp) return;
     const auto rs = rsrc_at(pool_pair + size_t(pg) * page_stride);
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
-      rw.s[m] = scales[size_t(pg) * hkv + 2 * pair + m];
-      const u32x2 a = __builtin_amdgcn_raw_buffer_load_b64(rs, off[0], m * page_bytes, 0);
+      if (!keys) rw.s[m] = vs_s[size_t(pg) * hkv + 2 * pair + m];
+      const u32x2 a = __builtin_amdgcn_raw_buffer_load_b64(rs, off, m * page_bytes, 0);
       if constexpr (T::B8 == 16) {
-        const u32x2 b = __builtin_amdgcn_raw_buffer_load_b64(rs, off[1], m * page_bytes, 0);
+        const u32x2 b = __builtin_amdgcn_raw_buffer_load_b64(rs, (keys ? off ^ 64u : off) + 4 * D, m * page_bytes, 0);
         rw.x[m] = u32x4{a.x, a.y, b.x, b.y};
       } else {
         rw.x[m] = u32x4{a.x, a.y, 0u, 0u};
       }
     }
   };
-  auto store8 = [&](int j0, int from, const Rows8& rw, uint8_t* dst, bool in_prefix) __attribute__((always_inline)) {
+  // `keys`: the codes are stored as they are
+  auto store8 = [&](int j0, int from, const Rows8& rw, uint8_t* dst, bool in_prefix, bool keys) __attribute__((always_inline)) {
     if (!in_prefix && (j0 + wrow0 >= lp || j0 + wrow0 + 7 < from)) return;
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
       const PageScale sc = page_scale(rw.s[m]);
+      auto widen = [&](uint32_t lo, uint32_t hi) { return keys ? fp8x8_f16x8(lo, hi) : fp8x8_f16x8(lo, hi, sc); };
       if constexpr (T::B8 == 16) {
-        if (in_prefix || j0 + r8[0] < lp)
-          *reinterpret_cast<u32x4*>(dst + m * T::TILE + wrow0 * T::RB + 16 * lane) = fp8x8_f16x8(rw.x[m].x, rw.x[m].y, sc);
-        if (in_prefix || j0 + r8[1] < lp)
-          *reinterpret_cast<u32x4*>(dst + m * T::TILE + (wrow0 + 4) * T::RB + 16 * lane) =
-              fp8x8_f16x8(rw.x[m].z, rw.x[m].w, sc);
-      } else if (in_prefix || j0 + r8[0] < lp) {
-        *reinterpret_cast<u32x4*>(dst + m * T::TILE + wrow0 * T::RB + 16 * lane) = fp8x8_f16x8(rw.x[m].x, rw.x[m].y, sc);
+        if (in_prefix || j0 + r8 < lp)
+          *reinterpret_cast<u32x4*>(dst + m * T::TILE + wrow0 * T::RB + 16 * lane) = widen(rw.x[m].x, rw.x[m].y);
+        if (in_prefix || j0 + r8 + 4 < lp)
+          *reinterpret_cast<u32x4*>(dst + m * T::TILE + (wrow0 + 4) * T::RB + 16 * lane) = widen(rw.x[m].z, rw.x[m].w);
+      } else if (in_prefix || j0 + r8 < lp) {
+        *reinterpret_cast<u32x4*>(dst + m * T::TILE + wrow0 * T::RB + 16 * lane) = widen(rw.x[m].x, rw.x[m].y);
       }
     }
   };
@@ -317,6 +331,12 @@ void diff_extend_kernel(DiffParams dp, PlanArg<AP> ap) {
         }
       }
   };
+
+  // fp8 pools: page (then key scale, of this wave's map) of the key group g of the key tile whose
+  // value tile starts at j0.  Behind the prefix: no page, scale unused.
+  auto group_key = [&](int j0, int g) { return j0 + kAhead + g * (BLOCK_N / T::KS); };
+  auto scale_page = [&](int key) -> int { return key < lp ? bt_s[key / P] : 0; };
+  auto key_scale = [&](int key, int pg) -> float { return key < lp ? ks_s[size_t(pg) * hkv + 2 * pair + map] : 1.f; };
 
   // ---- LDS fragment addresses (relative to a stage's matrix), as in the extend kernel
   uint32_t k_addr[T::KT];
@@ -364,11 +384,34 @@ void diff_extend_kernel(DiffParams dp, PlanArg<AP> ap) {
         if (k0 + 16 * (i >> 3) + 8 * h + (i & 7) >= lim) s[i] = -INFINITY;
     }
   };
+  // What the scores of the block in hand are multiplied with in the exponent: c, over fp8 pools
+  // times the scale of their page (of the keys of element group i / 8, which share one).
+  float cg[2] = {c, c};
+  // ... of the block of keys from k0 on, with scores s and page scales ks[0], ks[1].  Where the
+  // prefix ends among the 16 keys of a group, they are scaled in s.
+  auto set_scales = [&](float ks0, float ks1, int k0, Keys keys, f32x16& s) __attribute__((always_inline)) {
+    if constexpr (FP8) {
+      if (keys == Keys::kNew || (keys == Keys::kMasked && k0 >= lp)) {
+        cg[0] = cg[1] = c;
+        return;
+      }
+#pragma unroll
+      for (int gi = 0; gi < 2; ++gi) {
+        const float f = gi == 0 ? ks0 : ks1;
+        const int cached = lp - (k0 + 16 * gi);  // of these keys, where that is below 16
+        cg[gi] = keys == Keys::kPrefix || cached >= 16 ? c * f : c;
+        if (keys == Keys::kMasked && cached > 0 && cached < 16) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) s[8 * gi + e] *= 8 * h + e < cached ? f : 1.f;
+        }
+      }
+    }
+  };
   auto block_max = [&](const f32x16& x) -> float {
     float mx = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) mx = fmaxf(mx, x[i]);
-    return row_max(mx) * c;
+    for (int i = 0; i < 16; ++i) mx = fmaxf(mx, FP8 ? x[i] * cg[i >> 3] : x[i]);
+    return FP8 ? row_max(mx) : row_max(mx) * c;
   };
   auto weights = [&](const f32x16& x, u32x4(&pf)[2], float& lsum) __attribute__((always_inline)) {
     float la = 0.f, lb = 0.f;
@@ -376,7 +419,7 @@ void diff_extend_kernel(DiffParams dp, PlanArg<AP> ap) {
     for (int gi = 0; gi < 2; ++gi) {
       float w[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) w[e] = __builtin_amdgcn_exp2f(fmaf(x[8 * gi + e], c, -m_run));
+      for (int e = 0; e < 8; ++e) w[e] = __builtin_amdgcn_exp2f(fmaf(x[8 * gi + e], FP8 ? cg[gi] : c, -m_run));
       if constexpr (FP8) {
         const f16x2 one = {static_cast<_Float16>(1.f), static_cast<_Float16>(1.f)};
         f16x8 b;
@@ -426,7 +469,7 @@ void diff_extend_kernel(DiffParams dp, PlanArg<AP> ap) {
   };
   // One block of 32 keys: the next block's scores (rows 32 blk on of key tile kt, keys from
   // k_next on) while this block's weights are formed, then this block's values.
-  auto step = [&](const uint8_t* kt, const uint8_t* vt, int blk, int k_next, bool edge, f32x16& x,
+  auto step = [&](const uint8_t* kt, const uint8_t* vt, int blk, int k_next, Keys keys, const float (&ks)[T::KS], f32x16& x,
                   f32x16& s) __attribute__((always_inline)) {
     u32x4 pf[2];
     float lsum;
@@ -447,7 +490,8 @@ void diff_extend_kernel(DiffParams dp, PlanArg<AP> ap) {
     }
     l_run += lsum;
     if constexpr (D == 64) __builtin_amdgcn_s_setprio(0);
-    if (edge) mask(k_next, s);
+    set_scales(ks[blk * T::KS / 2], ks[blk * T::KS / 2 + T::KS / 4], k_next, keys, s);
+    if (keys == Keys::kMasked) mask(k_next, s);
     accumulate(vt, blk, pf);
   };
 
@@ -455,6 +499,27 @@ void diff_extend_kernel(DiffParams dp, PlanArg<AP> ap) {
   f32x16 xa = f32x16{}, xb = f32x16{};
   Rows8 k8{}, v8{};
   int pg_k = 0, pg_v = 0;  // pages of the tiles to be issued (fp8: loaded) next
+  float ks_next[T::KS];    // fp8: key scales of the tile of the next iteration, pages of the one after it
+  int pg_s[T::KS];
+#pragma unroll
+  for (int g2 = 0; g2 < T::KS; ++g2) {
+    ks_next[g2] = 1.f;
+    pg_s[g2] = 0;
+  }
+  // takes the key scales of iteration j's tile and loads those of the next one's
+  auto next_scales = [&](int j, float (&ks)[T::KS], bool in_prefix) __attribute__((always_inline)) {
+    if constexpr (FP8) {
+#pragma unroll
+      for (int g2 = 0; g2 < T::KS; ++g2) ks[g2] = ks_next[g2];
+      if (!in_prefix && group_key(tile0(j + 1), 0) >= lp) return;
+#pragma unroll
+      for (int g2 = 0; g2 < T::KS; ++g2) {
+        if (in_prefix) ks_next[g2] = ks_s[size_t(pg_s[g2]) * hkv + 2 * pair + map];
+        else ks_next[g2] = key_scale(group_key(tile0(j + 1), g2), pg_s[g2]);
+        pg_s[g2] = in_prefix ? bt_s[group_key(tile0(j + 2), g2) / P] : scale_page(group_key(tile0(j + 2), g2));
+      }
+    }
+  };
   __syncthreads();  // zero fill done before any tile lands
   {
     const int b0 = it.kv_begin;
@@ -467,23 +532,30 @@ void diff_extend_kernel(DiffParams dp, PlanArg<AP> ap) {
     pg_v = load_page(tile0(1));
     if constexpr (FP8) {
       Rows8 kp{}, kf{}, vf{};
-      if (wrow0 >= kAhead) load8(b0 - kAhead, pgp, k_pool_pair, ks_s, k8_off, kp, false);
-      load8(b0 + kAhead, pk0, k_pool_pair, ks_s, k8_off, kf, false);
-      load8(b0, pv0, v_pool_pair, vs_s, v8_off, vf, false);
+      if (wrow0 >= kAhead) load8(b0 - kAhead, pgp, k_pool_pair, k8_off, kp, false, true);
+      load8(b0 + kAhead, pk0, k_pool_pair, k8_off, kf, false, true);
+      load8(b0, pv0, v_pool_pair, v8_off, vf, false, false);
       __builtin_amdgcn_s_waitcnt(0);
-      if (wrow0 >= kAhead) store8(b0 - kAhead, b0, kp, lds_k1, false);
-      store8(b0 + kAhead, 0, kf, lds_k0, false);
-      store8(b0, 0, vf, lds_v0, false);
+      if (wrow0 >= kAhead) store8(b0 - kAhead, b0, kp, lds_k1, false, true);
+      store8(b0 + kAhead, 0, kf, lds_k0, false, true);
+      store8(b0, 0, vf, lds_v0, false, false);
       convert_new(b0 - kAhead, b0, lds_k1);
-      load8(tile0(1) + kAhead, pg_k, k_pool_pair, ks_s, k8_off, k8, false);
-      load8(tile0(1), pg_v, v_pool_pair, vs_s, v8_off, v8, false);
+      load8(tile0(1) + kAhead, pg_k, k_pool_pair, k8_off, k8, false, true);
+      load8(tile0(1), pg_v, v_pool_pair, v8_off, v8, false, false);
       pg_k = load_page(tile0(2) + kAhead);
       pg_v = load_page(tile0(2));
+#pragma unroll
+      for (int g2 = 0; g2 < T::KS; ++g2) {
+        ks_next[g2] = key_scale(group_key(b0, g2), scale_page(group_key(b0, g2)));
+        pg_s[g2] = scale_page(group_key(tile0(1), g2));
+      }
     }
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
     if (wave_active && b0 < wave_max_lim) {
       scores(lds_k1, 1, xa);
+      if constexpr (FP8)
+        set_scales(key_scale(b0, scale_page(b0)), key_scale(b0 + 16, scale_page(b0 + 16)), b0, Keys::kMasked, xa);
       mask(b0, xa);
       const float mx = block_max(xa);
       if (mx != -INFINITY) m_run = mx - kHeadroom;  // a row that sees none of these keys sees none of the item
@@ -500,23 +572,25 @@ void diff_extend_kernel(DiffParams dp, PlanArg<AP> ap) {
       convert_new(tile0(j), 0, v_cur);
     }
     __syncthreads();  // everyone's has; the other stages are no longer read
+    float ks[T::KS];
+    next_scales(j, ks, false);
     if (j + 1 < n_tiles) {
       if constexpr (FP8) {
-        store8(tile0(j + 1) + kAhead, 0, k8, k_nxt, false);
-        store8(tile0(j + 1), 0, v8, v_nxt, false);
+        store8(tile0(j + 1) + kAhead, 0, k8, k_nxt, false, true);
+        store8(tile0(j + 1), 0, v8, v_nxt, false, false);
       }
       issue(tile0(j + 1) + kAhead, 0, k_nxt, pg_k, k_pool, k_new, k_off, kn_off);
       issue(tile0(j + 1), 0, v_nxt, pg_v, v_pool, v_new, v_off, vn_off);
       if constexpr (FP8) {
-        load8(tile0(j + 2) + kAhead, pg_k, k_pool_pair, ks_s, k8_off, k8, false);
-        load8(tile0(j + 2), pg_v, v_pool_pair, vs_s, v8_off, v8, false);
+        load8(tile0(j + 2) + kAhead, pg_k, k_pool_pair, k8_off, k8, false, true);
+        load8(tile0(j + 2), pg_v, v_pool_pair, v8_off, v8, false, false);
       }
       pg_k = load_page(tile0(j + (FP8 ? 3 : 2)) + kAhead);
       pg_v = load_page(tile0(j + (FP8 ? 3 : 2)));
     }
     if (!wave_active || tile0(j) >= wave_max_lim) return;  // nothing visible from here on
-    step(k_cur, v_cur, 0, tile0(j) + 32, true, xa, xb);
-    step(k_cur, v_cur, 1, tile0(j) + 64, true, xb, xa);
+    step(k_cur, v_cur, 0, tile0(j) + 32, Keys::kMasked, ks, xa, xb);
+    step(k_cur, v_cur, 1, tile0(j) + 64, Keys::kMasked, ks, xb, xa);
   };
   // Iterations whose staged tiles lie wholly in the cached prefix (fp8: whose loaded tiles do
   // too): every row sees all their keys and a wave's rows come from one page, so they carry
@@ -534,11 +608,13 @@ void diff_extend_kernel(DiffParams dp, PlanArg<AP> ap) {
                     uint8_t* v_nxt) __attribute__((always_inline)) {
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
+    float ks[T::KS];
+    next_scales(j, ks, true);
     if constexpr (FP8) {
-      store8(tile0(j + 1) + kAhead, 0, k8, k_nxt, true);
-      store8(tile0(j + 1), 0, v8, v_nxt, true);
-      load8(tile0(j + 2) + kAhead, pg_k, k_pool_pair, ks_s, k8_off, k8, true);
-      load8(tile0(j + 2), pg_v, v_pool_pair, vs_s, v8_off, v8, true);
+      store8(tile0(j + 1) + kAhead, 0, k8, k_nxt, true, true);
+      store8(tile0(j + 1), 0, v8, v_nxt, true, false);
+      load8(tile0(j + 2) + kAhead, pg_k, k_pool_pair, k8_off, k8, true, true);
+      load8(tile0(j + 2), pg_v, v_pool_pair, v8_off, v8, true, false);
     } else {
       issue_prefix(k_nxt, pg_k, k_pool_pair, k_off);
       issue_prefix(v_nxt, pg_v, v_pool_pair, v_off);
@@ -546,8 +622,8 @@ void diff_extend_kernel(DiffParams dp, PlanArg<AP> ap) {
     pg_k = load_page(tile0(j + (FP8 ? 3 : 2)) + kAhead);
     pg_v = load_page(tile0(j + (FP8 ? 3 : 2)));
     if (!wave_active) return;
-    step(k_cur, v_cur, 0, 0, false, xa, xb);
-    step(k_cur, v_cur, 1, 0, false, xb, xa);
+    step(k_cur, v_cur, 0, 0, Keys::kPrefix, ks, xa, xb);
+    step(k_cur, v_cur, 1, 0, Keys::kPrefix, ks, xb, xa);
   };
   // Iterations whose staged tiles lie wholly among the new tokens and whose scores every
   // row of the workgroup sees.
@@ -569,15 +645,17 @@ void diff_extend_kernel(DiffParams dp, PlanArg<AP> ap) {
       convert_new(tile0(j), 0, v_cur);
     }
     __syncthreads();
+    const float ks[T::KS] = {};  // (new keys have none)
     issue_new(tile0(j + 1) + kAhead, k_nxt, k_new, kn_off);
     issue_new(tile0(j + 1), v_nxt, v_new, vn_off);
     if (!wave_active) return;
-    step(k_cur, v_cur, 0, 0, false, xa, xb);
-    step(k_cur, v_cur, 1, 0, false, xb, xa);
+    step(k_cur, v_cur, 0, 0, Keys::kNew, ks, xa, xb);
+    step(k_cur, v_cur, 1, 0, Keys::kNew, ks, xb, xa);
   };
   // (floors: the numerators may be negative)
   const int n_steady = min((lp - it.kv_begin - 96) >> 6, n_tiles - 1) - (FP8 ? 1 : 0);
-  const int new_begin = max(0, ((lp - it.kv_begin + 63) >> 6) - 1);
+  // (fp8: the scores' keys too, so that they take no page scale)
+  const int new_begin = max(0, FP8 ? (lp - it.kv_begin + 31) >> 6 : ((lp - it.kv_begin + 63) >> 6) - 1);
   const int first_lim = lp + it.q_row0 / G + 1;
   const int new_end = min(min((total_len - it.kv_begin - 96) >> 6, ((first_lim - it.kv_begin - 96) >> 6) + 1), n_tiles - 1);
   int j = 0;
