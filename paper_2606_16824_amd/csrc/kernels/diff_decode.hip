@@ -15,7 +15,7 @@
 // pipeline this is).  Bytes in flight per CU decide: 32 KB tiles (D = 128, bf16) in two
 // stages and two waves per CU, smaller ones in three stages and three or six waves:
 // 128-144 KB of LDS.  fp8 pools keep their codes in LDS and are widened exactly (keys to
-// bf16, values to fp16); a page's K scale of each map multiplies that map's scores, the V
+// bf16, values to fp16 or bf16); a page's K scale of each map multiplies that map's scores, the V
 // scales of the two halves multiply the weights (one set of weights per half).
 //
 // 48 decodes of 2k-32k keys, 4 key pairs of 128: bf16 pages 581 us (5.7 TB/s of K/V; a plain
@@ -23,6 +23,8 @@
 // One decode of 131072 keys: 94 us bf16, 62 us fp8; of 1700 keys 12.7 us, its two launches,
 // the page ids' and the tiles' latencies, and 1.7 us per tile.
 #include <hip/hip_runtime.h>
+
+#include <type_traits>
 
 #include "../cw_internal.h"
 #include "../plan_expand.h"
@@ -35,6 +37,12 @@ using namespace diff;
 
 constexpr int kScalarSearchSeqs = 8;  // up to here an item's sequence is searched by scalar loads
 constexpr int kKeys = 32;             // keys of a tile
+// Up to this ratio of a chunk's V scales, their products with the weights are held in fp16: a
+// column's largest weight is at least 2^kHeadroom, its product at least 1, and what fp16 drops of
+// any other (2^-25) at most 2^-25 of that.  Further apart (one page's scale may be far above the
+// others', without any weight on it) they are pairs of bf16: 48 decodes of 2k-32k keys 329 -> 346
+// us at D = 128, 314 -> 326 at 64.
+constexpr float kNearScales = 256.f;
 
 // 16 bytes per lane from global memory straight into LDS (lane l at LDS address m0 + 16 l),
 // nontemporal: every byte is read once.  Inline assembly, so that the compiler does not
@@ -166,20 +174,6 @@ __global__ __launch_bounds__(64) void diff_decode_kernel(DiffParams dp, PlanArg<
       }
     }
   }
-  // fp8: each half's largest V scale of the chunk is taken out of the weights (and multiplied
-  // back at the end), so that fp16 holds them whatever the scales' size
-  float vs_max[2] = {1.f, 1.f};
-  if constexpr (FP8) {
-#pragma unroll
-    for (int m = 0; m < 2; ++m) {
-      float x = lane < n_pages ? fabsf(my_vs[m]) : 0.f;
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) x = fmaxf(x, __shfl_xor(x, d));
-      vs_max[m] = x > 0.f ? x : 1.f;
-      my_vs[m] /= vs_max[m];
-    }
-  }
-
   // Q^T (B operand): this column's query.  bf16 pools: k-step kk holds dims 16 kk + 8 h + e;
   // fp8 pools read 16 dims per fragment, so k-steps 2 t and 2 t + 1 hold dims 32 t + 16 h +
   // 8 (kk & 1) + e.  And the new token's key, and what each lane needs at the end (values
@@ -246,6 +240,26 @@ __global__ __launch_bounds__(64) void diff_decode_kernel(DiffParams dp, PlanArg<
   const uint32_t lds_base = lds_addr(lds);
 #pragma unroll 1
   for (int t = 0; t < min(n_tiles, T::STAGES); ++t) issue_tile(t, lds_base + t * T::TILE);
+  // fp8: each half's largest V scale of the chunk is taken out of the weights (and multiplied
+  // back at the end), so that fp16 holds them whatever the scales' size; `wide`: they lie further
+  // apart than kNearScales, and weights times scales keep fp32's range.
+  float vs_max[2] = {1.f, 1.f};
+  bool wide = false;
+  if constexpr (FP8) {
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      const float x = lane < n_pages ? fabsf(my_vs[m]) : 0.f;
+      vs_max[m] = x;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) vs_max[m] = fmaxf(vs_max[m], __shfl_xor(vs_max[m], d));
+      wide |= __any(x > 0.f && x * kNearScales < vs_max[m]);
+    }
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      if (wide || vs_max[m] == 0.f) vs_max[m] = 1.f;
+      my_vs[m] = lane < n_pages ? my_vs[m] / vs_max[m] : 0.f;  // (a tile's end may lie behind the pages)
+    }
+  }
   float x_own = 0.f;  // the new token's score, under the first tiles' latency
   if (has_new) {
 #pragma unroll
@@ -255,7 +269,9 @@ __global__ __launch_bounds__(64) void diff_decode_kernel(DiffParams dp, PlanArg<
     x_own = row_sum(x_own) * c;
   }
 
-  auto compute = [&](int t, const uint8_t* st) __attribute__((always_inline)) {
+  // TWO: how the weights are given to the second product (below)
+  auto compute = [&](int t, const uint8_t* st, auto two) __attribute__((always_inline)) {
+    constexpr bool TWO = decltype(two)::value;
     const int j0 = kb + t * kKeys;
     f32x16 s = f32x16{}, s2 = f32x16{};
     const int R = swap_bits_2_3(col);  // row m of the block reads key swap(m)
@@ -346,37 +362,41 @@ __global__ __launch_bounds__(64) void diff_decode_kernel(DiffParams dp, PlanArg<
     l_run += tsum;
     // O^T += V^T P^T over the tile's two 16-key slices
     const int grp = lane >> 4, ri = lane & 15;
+    // Neither form of the weights adds to the output's own rounding.  TWO: a weight is the sum of
+    // two bf16 (2^-16), for a second MFMA; else (fp8 pools) fp16 (2^-11), which holds the codes
+    // exactly too.  One bf16 weight each: relative error 2.4e-3 instead of 1.7e-3, 1% less time
+    // over bf16 pages and none over fp8 pages.  TWO is the item's: a branch in the tile loop made
+    // the compiler copy O (48 decodes 368 us).
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
         const uint8_t* vt = st + (2 + half) * T::MAT;
-        // Neither form of the weights adds to the output's own rounding.  bf16 pools: a weight
-        // is the sum of two bf16 (2^-16), for a second MFMA; fp8 pools: fp16 (2^-11), which
-        // holds the codes exactly too.  One bf16 weight each: relative error 2.4e-3 instead of
-        // 1.7e-3, 1% less time over bf16 pages and none over fp8 pages.
         bf16x8 pf, pl;
         f16x8 ph;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          if constexpr (FP8) {
-            ph[e] = static_cast<_Float16>(w[8 * u + e] * vs[u][half]);
+          const float x = FP8 ? w[8 * u + e] * vs[u][half] : w[8 * u + e];
+          if constexpr (TWO) {
+            pf[e] = static_cast<__bf16>(x);
+            pl[e] = static_cast<__bf16>(x - static_cast<float>(pf[e]));
           } else {
-            pf[e] = static_cast<__bf16>(w[8 * u + e]);
-            pl[e] = static_cast<__bf16>(w[8 * u + e] - static_cast<float>(pf[e]));
+            ph[e] = static_cast<_Float16>(x);
           }
         }
 #pragma unroll
         for (int b = 0; b < T::DB; ++b) {
           f32x16& ob = o[half * T::DB + b];
+          u32x2 codes;
+          bf16x8 vf;
           if constexpr (FP8) {
             // source lane (k, a) = (ri / 2, ri % 2): key 16 u + 8 h + k, dims 32 b + 16 (grp & 1) + 8 a
             const int Rv = 16 * u + 8 * h + (ri >> 1);
             const int dbyte = 32 * b + 16 * (grp & 1) + 8 * (ri & 1);
             const int off = Rv * T::RB + 16 * ((dbyte >> 4) ^ v_swz8<T::RB>(Rv)) + (dbyte & 15);
             const i32x2 raw = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)(vt + off));
-            ob = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-                fp8x8_f16x8(u32x2{static_cast<uint32_t>(raw.x), static_cast<uint32_t>(raw.y)}), ph, ob, 0, 0, 0);
+            codes = u32x2{static_cast<uint32_t>(raw.x), static_cast<uint32_t>(raw.y)};
+            if constexpr (TWO) vf = fp8x8_bf16x8(codes);
           } else {
             const int kq = ri >> 2, a = ri & 3;
             const int chunk = 4 * b + 2 * (grp & 1) + (a >> 1);
@@ -387,19 +407,30 @@ __global__ __launch_bounds__(64) void diff_decode_kernel(DiffParams dp, PlanArg<
               const int off = Rv * T::RB + 16 * (chunk ^ v_swz16<T::RB>(Rv)) + 8 * (a & 1);
               part[e4] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(vt + off));
             }
-            const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
+            vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
+          }
+          if constexpr (TWO) {
             ob = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, ob, 0, 0, 0);
             ob = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pl, ob, 0, 0, 0);
+          } else {
+            ob = __builtin_amdgcn_mfma_f32_32x32x16_f16(fp8x8_f16x8(codes), ph, ob, 0, 0, 0);
           }
         }
       }
     }
-    if constexpr (!FP8) {  // (mask 0x100: LDS reads, 0x008: MFMAs) values' fragments three ahead
+    if constexpr (!FP8) {  // (mask 0x100: LDS reads, 0x008: MFMAs) values' fragments three ahead, fp8 two
       __builtin_amdgcn_sched_group_barrier(0x100, 6, 1);
 #pragma unroll
       for (int i = 0; i < 2 * T::VB; ++i) {
         __builtin_amdgcn_sched_group_barrier(0x008, 2, 1);
         __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
+      }
+    } else if constexpr (!TWO) {
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
+#pragma unroll
+      for (int i = 0; i < 2 * T::VB; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
       }
     }
   };
@@ -409,20 +440,24 @@ __global__ __launch_bounds__(64) void diff_decode_kernel(DiffParams dp, PlanArg<
   // instructions is a large part of its time (unrolled by the stages, with O exchanged and
   // the new value added in registers, a decode of one token alone took 13.8 us at D = 128
   // against 6.9, 48 decodes over bf16 pages 635 us against 615).
-  uint32_t off = 0;
+  auto tiles = [&](auto two) __attribute__((always_inline)) {
+    uint32_t off = 0;
 #pragma unroll 1
-  for (int t = 0; t < n_tiles; ++t) {
-    const int behind = n_tiles - 1 - t;
-    if (T::STAGES > 2 && behind >= 2) wait_vmcnt<(T::STAGES - 1) * T::DMA>();
-    else if (behind >= 1) wait_vmcnt<T::DMA>();
-    else wait_vmcnt<0>();
-    compute(t, lds + off);
-    if (behind >= T::STAGES) {
-      wait_lgkmcnt0();  // the stage's reads are done before it is refilled
-      issue_tile(t + T::STAGES, lds_base + off);
+    for (int t = 0; t < n_tiles; ++t) {
+      const int behind = n_tiles - 1 - t;
+      if (T::STAGES > 2 && behind >= 2) wait_vmcnt<(T::STAGES - 1) * T::DMA>();
+      else if (behind >= 1) wait_vmcnt<T::DMA>();
+      else wait_vmcnt<0>();
+      compute(t, lds + off, two);
+      if (behind >= T::STAGES) {
+        wait_lgkmcnt0();  // the stage's reads are done before it is refilled
+        issue_tile(t + T::STAGES, lds_base + off);
+      }
+      off = off == (T::STAGES - 1) * T::TILE ? 0u : off + T::TILE;
     }
-    off = off == (T::STAGES - 1) * T::TILE ? 0u : off + T::TILE;
-  }
+  };
+  if (FP8 && !wide) tiles(std::bool_constant<!FP8>{});
+  else tiles(std::true_type{});
   wait_vmcnt<0>();  // no DMA may land in LDS after the wave has ended
 
   // the new token's own key: its weight, and what it leaves of the others'
