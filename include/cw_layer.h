@@ -22,8 +22,13 @@ extern "C" {
 
 /* Block-table entries of a step's new pages and the index arrays of its new tokens,
  * from request lengths in *device* memory (CacheWise Sec. 2: KV prefixes persist in
- * fixed-size blocks, which a block table maps).  No length passes through the host,
- * so a captured call serves every step of up to max_tokens tokens.
+ * fixed-size blocks, which a block table maps).  No length passes through the host, so a
+ * captured call serves every step of up to max_tokens tokens.  It keeps no place in the free
+ * list: every call, and every replay of a captured one, takes pages from free_pages[0] on, so the
+ * program moves the list on by info[0] pages before the next one (which work captured behind the
+ * call can do).  For programs that keep their free pages in such a list; cw_bm_* (cw_policy.h)
+ * hands out tables of its own.  The calls that plan on the host (attention, cw_kv_write_pages) take
+ * their lengths there.  cu_rows and seq_ids are for the program's own kernels.
  *
  * With held_b = ceil(Lp_b / P) and need_b = ceil((Lp_b + Ls_b) / P):
  *   block_table[b][held_b + i] = free_pages[F_b + i],  0 <= i < need_b - held_b,
