@@ -50,8 +50,7 @@ __global__ __launch_bounds__(kThreads) void diff_combine_kernel(DiffParams dp, P
   const int lane = threadIdx.x % 64;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int lr = (blockIdx.x % wgs_per_group) * ROWS + wave / WPR;
-  if (WPR > 1 && lr >= cg.rows) return;  // (uniform over the workgroup: ROWS is 1)
-  if (lr >= cg.rows) return;
+  if (lr >= cg.rows) return;  // (where waves meet at a barrier, uniform over the workgroup: ROWS is 1)
   const int d0 = lane * PER;
   float m[2] = {-INFINITY, -INFINITY}, L[2] = {0.f, 0.f};
   vec acc[2] = {vec(0.f), vec(0.f)};
