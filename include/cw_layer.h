@@ -124,8 +124,9 @@ cw_status_t cw_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int6
  * takes q, k_new, v_new and the cached values (code * scale) in fp16: of such a call their
  * magnitudes must lie below 65504 (and are held to 2^-25 where they lie below 2^-14).  Key
  * scales are applied to the scores in fp32 by both.  The streaming kernel has no such limit:
- * V scales may differ as they like.  A scale may be 0 (a page of zeros).  With a norm, mean(x_h^2)
- * must be an fp32 number: values below about 2^59.  A NaN or infinity in a new token's value may
+ * V scales may differ as they like.  A scale may be 0 (a page of zeros).  Values (code *
+ * scale) lie below 2^80, as they are summed in fp32 with weights of up to 2^16; with a norm,
+ * mean(x_h^2) must be an fp32 number: values below about 2^59.  A NaN or infinity in a new token's value may
  * reach the rows of earlier tokens of its sequence (their weight for it is zero); what slots at or
  * past a prefix's end hold changes no result.  Lengths, plan, capture, aliasing and errors as for
  * cw_step_attention; the timing events are not recorded.  Workspace:
