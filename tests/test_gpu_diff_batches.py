@@ -63,3 +63,43 @@ def test_batch(singles, chunks, d, page, pairs, g, in_args, dt):
     over = np.abs(got - ref) / (r * terms["mass"] + 2.0 ** -8 * np.abs(ref))
     print(f"[batch] worst {over.max():.3f} of the tolerance over {len(ref)} rows", flush=True)
     assert np.isfinite(got).all() and over.max() <= 1.0
+
+
+@pytest.mark.parametrize("dt", ["bf16", "fp8"])
+def test_a_captured_batch_whose_plan_does_not_fit_the_arguments(dt):
+    """Replayed between eager calls of another batch on the same workspace."""
+    print(f"\n[case] captured diff batch {dt}", flush=True)
+    cwlib.init()
+    rng = np.random.default_rng(77)
+    lp, ls = _lens(rng, 400, 12)
+    calls = []
+    for a, b in ((lp, ls), (lp[:60], ls[:60])):
+        w = cw.materialize(cw.custom_spec(a.tolist(), b.tolist(), num_kv_heads=2, gqa_group=2, head_dim=64, page_size=16,
+                                          kv_dtype=dt, seed=len(a)))
+        dw = to_gpu(w)
+        calls.append((dw, torch.empty(dw.q.shape[0], 2, 128, dtype=torch.bfloat16, device="cuda")))
+    lam = torch.rand(2, generator=torch.Generator().manual_seed(1)).cuda()
+    ws = torch.empty(max(cwlib.diff_workspace_bytes(c.spec.prefix_lens, c.spec.suffix_lens, 1, 2, 64, 16, dt) for c, _ in calls),
+                     dtype=torch.uint8, device="cuda")
+
+    def run(i):
+        dw, out = calls[i]
+        s = dw.spec
+        return cwlib.diff_attention(dw.q, dw.k_new, dw.v_new, dw.k_pool, dw.v_pool, dw.block_table, s.prefix_lens,
+                                    s.suffix_lens, 2, s.softmax_scale, lam, k_scale=dw.k_scale, v_scale=dw.v_scale, out=out,
+                                    workspace=ws)
+
+    before = cwlib.arg_plan_calls()
+    want = run(0).clone()
+    assert cwlib.arg_plan_calls() == before
+    other = run(1).clone()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        run(0)
+    for rep in range(4):
+        calls[0][1].fill_(float("nan"))
+        again = run(1)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(again, other) and torch.equal(calls[0][1], want), rep
