@@ -18,10 +18,11 @@
 // bf16, values to fp16 or bf16); a page's K scale of each map multiplies that map's scores, the V
 // scales of the two halves multiply the weights (one set of weights per half).
 //
-// 48 decodes of 2k-32k keys, 4 key pairs of 128: bf16 pages 581 us (5.7 TB/s of K/V; a plain
-// copy moves 4.9 TB/s), fp8 pages 313 us (5.3 TB/s); 64-wide keys, 8 pairs: 516 and 285 us.
-// One decode of 131072 keys: 94 us bf16, 62 us fp8; of 1700 keys 12.7 us, its two launches,
-// the page ids' and the tiles' latencies, and 1.7 us per tile.
+// In a graph, 48 decodes of 2k-32k keys, 4 key pairs of 128: over 16-token pages bf16 604 us (5.7
+// TB/s of K/V; a plain copy moves 4.9), fp8 336 us (5.1), over 64-token pages 561 and 296; 8
+// pairs of 64: 598 and 323, over 64-token pages 550 and 314.  One decode of 131072 keys: 100 us
+// bf16, 64 us fp8; of 1700 keys 12.8 us, its two launches, the page ids' and the tiles'
+// latencies, and 1.7 us per tile.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>

@@ -30,10 +30,13 @@
 // see, run in loops without row checks and masks.  At D = 128 the two stages of both take
 // 128 KB of LDS, one workgroup per CU.
 //
-// Bound by the matrix cores: 4096 new tokens on 32768 cached ones, 8 key pairs of 4 query
-// pairs at D = 128, take 5.9-6.2 ms, 1139-1186 TFLOP/s (a plain bf16 product of 8192^3
-// reaches 1214); at D = 64 (half the matrix work per exponential) 1034-1070 TFLOP/s; over
-// fp8 pools, whose rows are widened on the way, 1000-1050 and 905-933.
+// 4096 new tokens on 32768 cached ones, 8 key pairs of 4 query pairs at D = 128, take 6.1 ms,
+// 1150 TFLOP/s, on a card where a plain bf16 product of 8192^3 reaches 1385 (cards differ: 5.9-6.5
+// ms, products 1214-1390); at D = 64 (half the matrix work per exponential) 1063 TFLOP/s; over fp8
+// pools, whose rows are widened on the way, 1031 and 932.  Bound by what surrounds the matrix
+// products: at D = 128 the matrix cores are busy 57% of the cycles and the waves wait 30% of
+// theirs, as every value fragment read from LDS (1.67 LDS instructions per MFMA) feeds one
+// product and a SIMD has two waves.
 #include <hip/hip_runtime.h>
 
 #include "../cw_internal.h"

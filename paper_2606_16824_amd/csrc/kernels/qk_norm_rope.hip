@@ -14,8 +14,8 @@
 // angles times the weights in registers over all heads that it takes (64 bytes of them
 // per 16 bytes of a head: read for each head they took a third of the loads), and issues
 // the loads of kBatch heads of each lane before it uses them.  GPU time of one token (32 + 8 +
-// 8 heads of 128, bf16 pages) 3.7 us, of 16384 tokens 94.9 us (5.0 TB/s; a plain copy moves
-// 4.9), of 1531 tokens of 64 + 8 heads without pages 15.2 us.
+// 8 heads of 128, bf16 pages) 3.6 us, of 16384 tokens 95 us (5.0 TB/s; a plain copy moves 4.9),
+// with fp8 pages 93, of 1531 tokens of 64 + 8 heads without pages 14.8 us.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

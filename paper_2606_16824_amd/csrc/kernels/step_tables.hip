@@ -14,8 +14,9 @@
 // the workspace first.  All arithmetic on lengths is in 32 bits, clipped, with shifts for the
 // page size: in 64 bits with divisions the largest steps were bound by it.  A page's and a
 // token's loads go out together, and a workgroup of its own sums `info`.  Time in a graph of 8
-// sequences 2.8 us (3.8 with `info` by the last workgroup and pages before tokens), of 200
-// with 25k tokens 4.2, of 3500 with 304k tokens 9.7 us (20.7 in 64 bits).
+// sequences 2.8-3.0 us (3.8 with `info` by the last workgroup and pages before tokens), of 200
+// with 25k tokens 4.2-4.5, of 3500 with 304k tokens 9.7-9.8 us (20.7 in 64 bits), of 9000 with 798k
+// tokens, in two launches, 36 us.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
