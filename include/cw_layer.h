@@ -1,8 +1,9 @@
 /*
  * cw_layer.h -- what a layer of a served model does around its attention over the
  * paged pools of cw.h: the tables of a step from lengths on the GPU, the norm and
- * position rotation of queries and keys with the page write, and differential
- * attention.
+ * position rotation of queries and keys with the page write (one position per token, or
+ * one for each of several axes), the norms around the residual stream, differential
+ * attention, and attention with shaped scores.
  *
  * Ownership, ordering, errors and graph capture are those of cw.h: the caller owns
  * every buffer, work is enqueued on `stream`, every argument is checked before
@@ -98,6 +99,96 @@ cw_status_t cw_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int6
                             const float* k_scale, const float* v_scale, const int64_t* slots,
                             int32_t num_pages, int32_t page_size, cw_kv_dtype_t kv_dtype,
                             hipStream_t stream);
+
+/* cw_qk_norm_rope for positions with several axes (time, height and width of an image or a
+ * video): pair i of a head (0 <= i < R / 2) is rotated by the cos and sin of column i at the
+ * token's position on axis axis_of_h[i].  All else as cw_qk_norm_rope.
+ *
+ * positions: device int32 [num_axes, T]; a token one of whose positions lies outside [0,
+ * num_positions) is not written, like one without a position there.  num_axes 1..4; axis_of_h:
+ * host int32 [R / 2], each in 0 .. num_axes - 1, read before the call returns. */
+cw_status_t cw_qk_norm_rope_axes(const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                                 const void* v, int64_t v_stride, int32_t num_tokens,
+                                 int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                                 const float* q_weight, const float* k_weight, float eps,
+                                 const float* cos_sin, int32_t num_positions, int32_t rotary_dim,
+                                 int32_t interleaved, const int32_t* positions, int32_t num_axes,
+                                 const int32_t* axis_of_h, void* q_out, void* k_out, void* v_out,
+                                 void* k_pool, void* v_pool, const float* k_scale,
+                                 const float* v_scale, const int64_t* slots, int32_t num_pages,
+                                 int32_t page_size, cw_kv_dtype_t kv_dtype, hipStream_t stream);
+
+/* The norm of a block's output, its gate, the scaled residual stream and the norm before the
+ * next block, in one pass over a token's row of `width` elements:
+ *   u  = x / sqrt(mean(x^2) + eps) * post_weight           (post_weight NULL: u = x)
+ *   r' = residual_scale * residual + gate * u              (gate NULL: 1)
+ *   y  = r' / sqrt(mean(r'^2) + eps) * pre_weight          (pre_weight and y_out NULL: no y)
+ * in fp32; r' is rounded once to residual_out's type, y once to bf16, from r' before its
+ * rounding.  mean(x^2) and mean(r'^2) must be fp32 numbers (values below about 2^56).
+ *
+ * x bf16 [T, width], x_stride elements from one token to the next; residual and residual_out
+ * contiguous [T, width], bf16 or (residual_fp32 != 0) fp32; y_out bf16 contiguous; post_weight,
+ * pre_weight fp32 [width]; gate bf16 [width] for all tokens (gate_stride 0) or a row for each,
+ * gate_stride elements apart.  width a multiple of 8 in 8 .. 16384, strides multiples of 8, eps
+ * finite and >= 0, residual_scale finite, 16-byte alignment of every tensor.  residual_out may
+ * be residual; outputs overlap nothing else (CW_ERR_ALIAS).  No workspace; needs no cw_init. */
+cw_status_t cw_residual_norm(const void* x, int64_t x_stride, const void* residual,
+                             int32_t residual_fp32, int32_t num_tokens, int32_t width,
+                             const float* post_weight, const void* gate, int64_t gate_stride,
+                             float residual_scale, const float* pre_weight, float eps,
+                             void* residual_out, void* y_out, hipStream_t stream);
+
+/* Attention with shaped scores over the paged cache: scores capped by a tanh, biased by
+ * distance, and masked by a window, by documents or by a prefix whose tokens all see each
+ * other; for chunks of new tokens and single tokens mixed.  For the new token at position p of
+ * its sequence, its query head h and key j:
+ *   x_j = softmax_scale q.k_j
+ *   x_j <- score_cap tanh(x_j / score_cap)                 (score_cap 0: no cap)
+ *   x_j <- x_j - slopes[h] |p - j|                         (slopes NULL: no bias)
+ *   out = sum_j softmax(x)_j v_j over the visible keys j, lse = ln sum_j exp(x_j)
+ * Key j is visible where all of these hold:
+ *   j <= p, or j < full_lens_h[b]: the first full_lens_h[b] tokens of sequence b see each other
+ *     (NULL: none do; what lies beyond the sequence's last token counts for nothing).  Tokens
+ *     of that prefix that earlier calls cached have seen only what was there then;
+ *   j > p - window                                         (window 0: no limit);
+ *   j >= key_begins[t], the first visible position of new token t, such as the start of its
+ *     document (NULL, or negative: 0).
+ * A token that sees no key gets out = 0 and lse = -inf.  With neither of them the call is the
+ * attention of cw_step_attention without its page write: the pools are only read.
+ *
+ * Tensors, pools, scales, block table and lengths as for cw_extend_attention; out bf16 [T, Hq,
+ * D], lse fp32 [T, Hq] or NULL; slopes device fp32 [Hq], any finite values; key_begins device
+ * int32 [T]; full_lens_h host int32 [num_seqs].  score_cap 0 or 2^-10 .. 4096; a capped score is
+ * held to score_cap * 2^-20.  Block-table entries of pages that lie wholly before the windows of
+ * all new tokens of their sequence are not read, nor is what those pages hold: a program may
+ * have given them away.
+ *
+ * Supported: head_dim 64 or 128, page_size 16 or 64, gqa_group 1..16, num_kv_heads 1..1024.
+ * Sequences with one new token run on an HBM-streaming kernel, the others on a matrix-core
+ * kernel, which over fp8 pools takes q, k_new, v_new and the cached values (code * scale) in
+ * fp16: of such a call their magnitudes must lie below 65504 (and are held to 2^-25 where they
+ * lie below 2^-14).  Key scales are applied to the scores in fp32 by both; a scale may be 0.
+ * Values (code * scale) lie below 2^80.  A NaN or infinity in a value that some row of a chunk
+ * sees may reach the rows of its sequence that do not (their weight for it is zero); what slots
+ * at or past a prefix's end hold changes no result.  Lengths, plan, capture, aliasing and
+ * errors as for cw_step_attention; the timing events are not recorded.  The plan depends on
+ * window and full_lens_h, not on the other shapes.  Workspace: cw_shaped_workspace_bytes (0 if the
+ * arguments are invalid). */
+size_t cw_shaped_workspace_bytes(const int32_t* prefix_lens_h, const int32_t* suffix_lens_h,
+                                 int32_t num_seqs, int32_t num_kv_heads, int32_t gqa_group,
+                                 int32_t head_dim, int32_t page_size, cw_kv_dtype_t kv_dtype,
+                                 int32_t window, const int32_t* full_lens_h);
+cw_status_t cw_shaped_attention(const void* q, const void* k_new, const void* v_new,
+                                const void* k_pool, const void* v_pool, const float* k_scale,
+                                const float* v_scale, const int32_t* block_table,
+                                int32_t bt_stride, int32_t num_pages,
+                                const int32_t* prefix_lens_h, const int32_t* suffix_lens_h,
+                                int32_t num_seqs, int32_t num_kv_heads, int32_t gqa_group,
+                                int32_t head_dim, int32_t page_size, float softmax_scale,
+                                cw_kv_dtype_t kv_dtype, float score_cap, const float* slopes,
+                                int32_t window, const int32_t* key_begins,
+                                const int32_t* full_lens_h, void* out, float* lse,
+                                void* workspace, size_t workspace_bytes, hipStream_t stream);
 
 /* Differential attention over the paged cache: the difference of two softmax maps with a
  * learned weight per head, for chunks of new tokens and single tokens mixed.

@@ -7,6 +7,9 @@ norm_rotate      RMS norm of head rows and their position rotation
 diff_attention   the difference of two softmax maps per query pair over a paged cache:
                  query heads 2h, 2h+1 against key heads 2j, 2j+1 of pair j = h // G, the value
                  of pair j being value heads 2j and 2j+1 side by side
+axis_angles      cos and sin of every token's rotated pairs where the pairs follow several position axes
+residual_norm    the norm of a block's output, its gate, the residual stream and the next norm
+shaped_attention softmax attention over a paged cache with capped, biased and masked scores
 """
 from __future__ import annotations
 
@@ -96,3 +99,68 @@ def diff_attention(inp: PagedInputs, lam: np.ndarray, weight: Optional[np.ndarra
     if weight is not None:
         out = x / np.sqrt((x * x).mean(axis=-1, keepdims=True) + eps) * weight.astype(np.float64)
     return out * out_scale, {"x": x, "mass": mass, "scores": scores}
+
+
+def axis_angles(cos_sin: np.ndarray, positions: np.ndarray, axis_of):
+    """(cos, sin) float64 [T, R / 2] from the table [positions, R], the positions [axes, T] and each pair's axis."""
+    half = cos_sin.shape[1] // 2
+    cos, sin = np.empty((positions.shape[1], half)), np.empty((positions.shape[1], half))
+    for i in range(half):
+        row = positions[axis_of[i]]
+        cos[:, i], sin[:, i] = cos_sin[row, i], cos_sin[row, half + i]
+    return cos, sin
+
+
+def residual_norm(x, residual, post=None, gate=None, scale: float = 1.0, pre=None, eps: float = 0.0):
+    """(residual, y) in float64, not rounded; y None without pre."""
+    def normed(z, w):
+        return z / np.sqrt((z * z).mean(axis=-1, keepdims=True) + eps) * np.asarray(w, dtype=np.float64)
+
+    u = np.asarray(x, dtype=np.float64)
+    u = u if post is None else normed(u, post)
+    r = scale * np.asarray(residual, dtype=np.float64) + (u if gate is None else np.asarray(gate, dtype=np.float64) * u)
+    return r, None if pre is None else normed(r, pre)
+
+
+def shaped_attention(inp: PagedInputs, cap: float = 0.0, slopes: Optional[np.ndarray] = None, window: int = 0,
+                     begins: Optional[np.ndarray] = None, full: Optional[np.ndarray] = None):
+    """(out [T, Hq, D], lse [T, Hq], terms): terms holds, for error bounds, `mass` (sum of weights times
+    |values|), `scores` (per row, the largest scale * sum |q| |k| of a visible key) and `bias` (per row, the
+    largest |bias| of one).  A row that sees nothing: 0 and -inf."""
+    total, hq, d = inp.q.shape
+    g = inp.gqa_group
+    out, lse = np.zeros((total, hq, d)), np.full((total, hq), -np.inf)
+    mass, scores, biases = np.zeros_like(out), np.zeros((total, hq, 1)), np.zeros((total, hq, 1))
+    cu = inp.cu()
+    q = bf16_bits_to_f64(inp.q)
+    for b in range(len(inp.prefix_lens)):
+        k, v = gather_sequence_kv(inp, b)
+        lp, ls = int(inp.prefix_lens[b]), int(inp.suffix_lens[b])
+        for i in range(ls):
+            row, p = int(cu[b]) + i, lp + i
+            j = np.arange(lp + ls)
+            seen = j <= p
+            if full is not None:
+                seen |= j < int(full[b])
+            if window:
+                seen &= j > p - window
+            if begins is not None:
+                seen &= j >= int(begins[row])
+            j = j[seen]
+            if len(j) == 0:
+                continue
+            for h in range(hq):
+                kj, vj = k[j, h // g], v[j, h // g]
+                x = inp.softmax_scale * (kj @ q[row, h])
+                if cap:
+                    x = cap * np.tanh(x / cap)
+                away = np.zeros(len(j)) if slopes is None else float(slopes[h]) * np.abs(p - j)
+                x = x - away
+                top = x.max()
+                w = np.exp(x - top)
+                lse[row, h] = top + np.log(w.sum())
+                w /= w.sum()
+                out[row, h], mass[row, h] = w @ vj, w @ np.abs(vj)
+                scores[row, h, 0] = (inp.softmax_scale * (np.abs(kj) @ np.abs(q[row, h]))).max()
+                biases[row, h, 0] = np.abs(away).max()
+    return out, lse, {"mass": mass, "scores": scores, "bias": biases}

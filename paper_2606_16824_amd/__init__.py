@@ -14,8 +14,10 @@ fallback: without the built library every call raises.
                    suffix_lens, k_scale=None, v_scale=None, workspace=None)
 
 and, of include/cw_layer.h, what a layer does around its attention: build_step_tables
-(block table and slots from lengths on the GPU), qk_norm_rope (norm, rotation and page
-write) and diff_attention (differential attention over pools of paired heads).
+(block table and slots from lengths on the GPU), qk_norm_rope and qk_norm_rope_axes (norm,
+rotation by one or several position axes, and page write), residual_norm (the norms around the
+residual stream), diff_attention (differential attention over pools of paired heads) and
+shaped_attention (capped, biased and masked scores).
 
 Page size and head dim are read from the pool shape [num_pages, Hkv, P, D];
 an fp8 pool is a uint8 (or float8_e4m3fn) tensor of e4m3fn codes.
@@ -42,7 +44,8 @@ __all__ = ["CWError", "init", "pinned_allocations", "arg_plan_calls", "extend_at
            "set_tuning", "plan_items", "decode_plan", "library", "kv_swap_out", "kv_swap_in", "swap_workspace_bytes",
            "step_attention", "step_workspace_bytes", "check_block_table", "ceiling_mfma_bf16", "ceiling_stream_read",
            "ceiling_stream_copy", "build_step_tables", "step_tables_workspace_bytes", "StepTables", "qk_norm_rope",
-           "diff_attention", "diff_workspace_bytes"]
+           "diff_attention", "diff_workspace_bytes", "qk_norm_rope_axes", "residual_norm", "shaped_attention",
+           "shaped_workspace_bytes"]
 
 
 class CWError(RuntimeError):
@@ -579,7 +582,7 @@ def _head_rows(t, name, total, heads, d):
 
 
 def _quick_rope(dev, total, hq, hkv, d, q, k, v, cos_sin, positions, weights, q_out, k_out, v_out, k_pool, v_pool, slots,
-                k_scale, v_scale):
+                k_scale, v_scale, pos_shape):
     """Whether every check of qk_norm_rope passes (else they are made one at a time)."""
     bf, f32 = torch.bfloat16, torch.float32
     rows_q, rows = (total, hq, d), (total, hkv, d)
@@ -591,7 +594,7 @@ def _quick_rope(dev, total, hq, hkv, d, q, k, v, cos_sin, positions, weights, q_
                 and q_out.dtype is bf and q_out.shape == rows_q and q_out.get_device() == dev and q_out.is_contiguous()
                 and k_out.dtype is bf and k_out.shape == rows and k_out.get_device() == dev and k_out.is_contiguous()
                 and cos_sin.dtype is f32 and cos_sin.dim() == 2 and cos_sin.get_device() == dev and cos_sin.is_contiguous()
-                and positions.dtype is torch.int32 and positions.shape == (total,) and positions.get_device() == dev
+                and positions.dtype is torch.int32 and positions.shape == pos_shape and positions.get_device() == dev
                 and positions.is_contiguous()):
             return False
         if v is not None:
@@ -623,14 +626,14 @@ def _quick_rope(dev, total, hq, hkv, d, q, k, v, cos_sin, positions, weights, q_
 
 
 def _check_rope(total, hq, hkv, d, q, k, v, cos_sin, positions, q_weight, k_weight, q_out, k_out, v_out, k_pool, v_pool,
-                slots, k_scale, v_scale):
+                slots, k_scale, v_scale, pos_shape):
     """The checks of qk_norm_rope, one at a time."""
     for x, name, h in ((q, "q", hq), (k, "k", hkv), (v, "v", hkv)):
         if x is not None:
             _head_rows(x, name, total, h, d)
     if not isinstance(cos_sin, torch.Tensor) or cos_sin.dim() != 2 or cos_sin.dtype != torch.float32:
         raise ValueError("cos_sin must be a 2-D float32 tensor [positions, rotary_dim]")
-    _want(positions, "positions", (torch.int32,), (total,))
+    _want(positions, "positions", (torch.int32,), pos_shape)
     for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
         if w is not None:
             _want(w, name, (torch.float32,), (d,))
@@ -660,6 +663,20 @@ def qk_norm_rope(q, k, cos_sin, positions, q_weight=None, k_weight=None, eps=1e-
     """Norm of every query and key head, position rotation and (with pools) page write in one
     pass (cw_qk_norm_rope).  q [T, Hq, D], k, v [T, Hkv, D] may be columns of one projection's
     output.  Returns (q_out, k_out, v_out), contiguous; v_out is None without v."""
+    return _norm_rope(None, q, k, cos_sin, positions, q_weight, k_weight, eps, interleaved, v, k_pool, v_pool, slots, k_scale,
+                      v_scale, q_out, k_out, v_out)
+
+
+def qk_norm_rope_axes(q, k, cos_sin, positions, axis_of, q_weight=None, k_weight=None, eps=1e-6, interleaved=False, v=None,
+                      k_pool=None, v_pool=None, slots=None, k_scale=None, v_scale=None, q_out=None, k_out=None, v_out=None):
+    """qk_norm_rope for positions with several axes (cw_qk_norm_rope_axes): positions int32 [axes, T], and
+    axis_of (host, rotary_dim / 2 entries) the axis that each rotated pair follows."""
+    return _norm_rope(_lens(axis_of), q, k, cos_sin, positions, q_weight, k_weight, eps, interleaved, v, k_pool, v_pool, slots,
+                      k_scale, v_scale, q_out, k_out, v_out)
+
+
+def _norm_rope(axis_of, q, k, cos_sin, positions, q_weight, k_weight, eps, interleaved, v, k_pool, v_pool, slots, k_scale,
+               v_scale, q_out, k_out, v_out):
     if not isinstance(q, torch.Tensor) or q.dim() != 3 or not isinstance(k, torch.Tensor) or k.dim() != 3:
         raise ValueError("q and k must be 3-D tensors [T, heads, D]")
     total, hq, d = q.shape
@@ -670,10 +687,18 @@ def qk_norm_rope(q, k, cos_sin, positions, q_weight=None, k_weight=None, eps=1e-
         k_out = new(hkv) if k_out is None else k_out
         v_out = new(hkv) if v is not None and v_out is None else v_out
     dev = torch._C._cuda_getDevice()
+    axes, pos_shape = 0, (total,)
+    if axis_of is not None:
+        if not isinstance(positions, torch.Tensor) or positions.dim() != 2:
+            raise ValueError("positions must be a 2-D int32 tensor [axes, T]")
+        axes = positions.shape[0]
+        pos_shape = (axes, total)
     if not _quick_rope(dev, total, hq, hkv, d, q, k, v, cos_sin, positions, (q_weight, k_weight), q_out, k_out, v_out,
-                       k_pool, v_pool, slots, k_scale, v_scale):
+                       k_pool, v_pool, slots, k_scale, v_scale, pos_shape):
         _check_rope(total, hq, hkv, d, q, k, v, cos_sin, positions, q_weight, k_weight, q_out, k_out, v_out, k_pool, v_pool,
-                    slots, k_scale, v_scale)
+                    slots, k_scale, v_scale, pos_shape)
+    if axis_of is not None and axis_of.shape != (cos_sin.shape[1] // 2,):
+        raise ValueError(f"axis_of has shape {axis_of.shape}, expected {(cos_sin.shape[1] // 2,)}")
     vp = vs = vo = kp = vpool = sl = ks = vsc = None
     num_pages, page, dt = 0, 0, L.CW_KV_BF16
     if v is not None:
@@ -683,13 +708,69 @@ def qk_norm_rope(q, k, cos_sin, positions, q_weight=None, k_weight=None, eps=1e-
         kp, vpool, sl = k_pool.data_ptr(), v_pool.data_ptr(), slots.data_ptr()
         if k_scale is not None:
             dt, ks, vsc = L.CW_KV_FP8_E4M3FN, k_scale.data_ptr(), v_scale.data_ptr()
-    _check(library().cw_qk_norm_rope(
-        q.data_ptr(), q.stride(0) if total > 1 else hq * d, k.data_ptr(), k.stride(0) if total > 1 else hkv * d, vp, vs or 0,
-        total, hq, hkv, d, None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr(),
-        eps, cos_sin.data_ptr(), cos_sin.shape[0], cos_sin.shape[1], 1 if interleaved else 0, positions.data_ptr(),
-        q_out.data_ptr(), k_out.data_ptr(), vo, kp, vpool, ks, vsc, sl, num_pages, page, dt,
-        torch._C._cuda_getCurrentRawStream(dev)))
+    head = (q.data_ptr(), q.stride(0) if total > 1 else hq * d, k.data_ptr(), k.stride(0) if total > 1 else hkv * d, vp,
+            vs or 0, total, hq, hkv, d, None if q_weight is None else q_weight.data_ptr(),
+            None if k_weight is None else k_weight.data_ptr(), eps, cos_sin.data_ptr(), cos_sin.shape[0], cos_sin.shape[1],
+            1 if interleaved else 0, positions.data_ptr())
+    tail = (q_out.data_ptr(), k_out.data_ptr(), vo, kp, vpool, ks, vsc, sl, num_pages, page, dt,
+            torch._C._cuda_getCurrentRawStream(dev))
+    if axis_of is None:
+        _check(library().cw_qk_norm_rope(*head, *tail))
+    else:
+        _check(library().cw_qk_norm_rope_axes(*head, axes, _ptr(axis_of), *tail))
     return q_out, k_out, v_out
+
+
+def _rows(t, name, total, width):
+    """Pointer and token stride of a bf16 [T, width] tensor with contiguous rows."""
+    _want(t, name, _BF16, (total, width))
+    if not t.is_cuda:
+        raise ValueError("tensors must be on the GPU")
+    if t.stride(1) != 1 and width > 1:
+        raise ValueError(f"{name}: a token's elements must be contiguous (strides {t.stride()})")
+    return t.data_ptr(), t.stride(0) if total > 1 else width
+
+
+def residual_norm(x, residual, post_weight=None, gate=None, residual_scale=1.0, pre_weight=None, eps=1e-6, residual_out=None,
+                  y_out=None):
+    """The norm of a block's output x [T, width] (with post_weight), its gate ([width], or [T, width]) and the scaled
+    residual stream (bf16 or fp32), and with pre_weight the norm before the next block, in one pass
+    (cw_residual_norm).  Returns (residual_out, y_out); y_out is None without pre_weight."""
+    if not isinstance(x, torch.Tensor) or x.dim() != 2:
+        raise ValueError("x must be a 2-D tensor [T, width]")
+    total, width = x.shape
+    xp, xs = _rows(x, "x", total, width)
+    _want(residual, "residual", (torch.bfloat16, torch.float32), (total, width))
+    if residual_out is None:
+        residual_out = torch.empty_like(residual)
+    else:
+        _want(residual_out, "residual_out", (residual.dtype,), (total, width))
+    if pre_weight is None:
+        if y_out is not None:
+            raise ValueError("y_out without pre_weight")
+    elif y_out is None:
+        y_out = torch.empty(total, width, dtype=torch.bfloat16, device=x.device)
+    else:
+        _want(y_out, "y_out", _BF16, (total, width))
+    for w, name in ((post_weight, "post_weight"), (pre_weight, "pre_weight")):
+        if w is not None:
+            _want(w, name, (torch.float32,), (width,))
+    gp, gs = None, 0
+    if gate is not None:
+        if isinstance(gate, torch.Tensor) and gate.dim() == 1:
+            _want(gate, "gate", _BF16, (width,))
+            gp = _dptr(gate)
+        else:
+            gp, gs = _rows(gate, "gate", total, width)
+    dev = torch._C._cuda_getDevice()
+    for t in (x, residual, residual_out, y_out, post_weight, pre_weight, gate):
+        if t is not None and t.get_device() != dev:
+            _one_device(x, residual, residual_out, y_out, post_weight, pre_weight, gate)
+    _check(library().cw_residual_norm(
+        xp, xs, _dptr(residual), 1 if residual.dtype is torch.float32 else 0, total, width, _dptr(post_weight), gp, gs,
+        float(residual_scale), _dptr(pre_weight), float(eps), _dptr(residual_out), _dptr(y_out),
+        torch._C._cuda_getCurrentRawStream(dev)))
+    return residual_out, y_out
 
 
 def diff_workspace_bytes(prefix_lens, suffix_lens, num_kv_pairs, gqa_group, head_dim, page_size,
@@ -730,6 +811,63 @@ def diff_attention(q, k_new, v_new, k_pool, v_pool, block_table, prefix_lens, su
         _dptr(block_table), block_table.shape[1], num_pages, _ptr(lp), _ptr(ls), len(lp), heads // 2, gqa_group, d,
         page, float(softmax_scale), _kv_dtype(k_pool), _dptr(lam), _dptr(norm_weight), float(norm_eps),
         float(out_scale), _dptr(out), _dptr(workspace), workspace.numel(), _stream()))
+    return out
+
+
+def _window(window) -> int:
+    window = int(window)
+    if not 0 <= window < 1 << 31:
+        raise ValueError(f"window = {window} must be in 0 .. 2^31 - 1")
+    return window
+
+
+def _full_lens(full_lens, num_seqs):
+    if full_lens is None:
+        return None
+    full = _lens(full_lens)
+    if full.shape != (num_seqs,):
+        raise ValueError(f"full_lens has shape {full.shape}, expected {(num_seqs,)}")
+    return full
+
+
+def shaped_workspace_bytes(prefix_lens, suffix_lens, num_kv_heads, gqa_group, head_dim, page_size, kv_dtype="bf16",
+                           window=0, full_lens=None) -> int:
+    lp, ls = _lens_pair(prefix_lens, suffix_lens)
+    full = _full_lens(full_lens, len(lp))
+    return int(library().cw_shaped_workspace_bytes(_ptr(lp), _ptr(ls), len(lp), num_kv_heads, gqa_group, head_dim,
+                                                   page_size, _dtype_code(kv_dtype), _window(window), _ptr(full)))
+
+
+def shaped_attention(q, k_new, v_new, k_pool, v_pool, block_table, prefix_lens, suffix_lens, gqa_group, softmax_scale,
+                     score_cap=0.0, slopes=None, window=0, key_begins=None, full_lens=None, k_scale=None, v_scale=None,
+                     out=None, lse=None, workspace=None):
+    """Attention over the paged cache with capped, biased and masked scores (cw_shaped_attention): score_cap of
+    a tanh, slopes fp32 [Hq] of a bias by distance, window in tokens, key_begins int32 [T] (first visible position
+    of each new token) and full_lens (host, per sequence: its first tokens all see each other).  The pools are
+    only read."""
+    lp, ls = _lens_pair(prefix_lens, suffix_lens)
+    total = _total(ls)
+    num_pages, hkv, page, d = _check_call(q, k_new, v_new, k_pool, v_pool, block_table, len(lp), total, gqa_group,
+                                          k_scale, v_scale, out, lse)
+    if out is None:
+        out = torch.empty_like(q)
+    full = _full_lens(full_lens, len(lp))
+    if slopes is not None:
+        _want(slopes, "slopes", (torch.float32,), (hkv * int(gqa_group),))
+    if key_begins is not None:
+        _want(key_begins, "key_begins", (torch.int32,), (total,))
+    dev = torch._C._cuda_getDevice()
+    if not (q.get_device() == dev == out.get_device() and (slopes is None or slopes.get_device() == dev)
+            and (key_begins is None or key_begins.get_device() == dev)):
+        _one_device(q, out, slopes, key_begins)
+    if workspace is None:
+        workspace = _workspace(shaped_workspace_bytes(lp, ls, hkv, gqa_group, d, page, _kv_dtype(k_pool), window, full),
+                               q.device, None)
+    _check(library().cw_shaped_attention(
+        _dptr(q), _dptr(k_new), _dptr(v_new), _dptr(k_pool), _dptr(v_pool), _dptr(k_scale), _dptr(v_scale),
+        _dptr(block_table), block_table.shape[1], num_pages, _ptr(lp), _ptr(ls), len(lp), hkv, gqa_group, d, page,
+        float(softmax_scale), _kv_dtype(k_pool), float(score_cap), _dptr(slopes), _window(window), _dptr(key_begins),
+        _ptr(full), _dptr(out), _dptr(lse), _dptr(workspace), workspace.numel(), _stream()))
     return out
 
 

@@ -79,6 +79,15 @@ SIGNATURES = {
     "cw_diff_attention": (C.c_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _vp, _vp, _i32, _i32, _i32,
                                     _i32, _i32, C.c_float, C.c_int, _vp, _vp, C.c_float, C.c_float, _vp, _vp, _sz,
                                     _vp]),
+    "cw_qk_norm_rope_axes": (C.c_int, [_vp, _i64, _vp, _i64, _vp, _i64, _i32, _i32, _i32, _i32, _vp, _vp, C.c_float,
+                                       _vp, _i32, _i32, _i32, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
+                                       _i32, _i32, C.c_int, _vp]),
+    "cw_residual_norm": (C.c_int, [_vp, _i64, _vp, _i32, _i32, _i32, _vp, _vp, _i64, C.c_float, _vp, C.c_float, _vp,
+                                   _vp, _vp]),
+    "cw_shaped_workspace_bytes": (_sz, [_vp, _vp, _i32, _i32, _i32, _i32, _i32, _i32, _i32, _vp]),
+    "cw_shaped_attention": (C.c_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _vp, _vp, _i32, _i32, _i32,
+                                      _i32, _i32, C.c_float, C.c_int, C.c_float, _vp, _i32, _vp, _vp, _vp, _vp, _vp,
+                                      _sz, _vp]),
     # include/cw_policy.h (host-only)
     "cw_policy_simulate": (C.c_int, [_vp, _vp, _vp, _vp, C.c_int64]),
     "cw_policy_predict": (C.c_int, [_vp, _i32, C.c_double, _vp]),

@@ -550,7 +550,8 @@ class LastPlan {
  public:
   template <class Make, class Bytes>
   std::shared_ptr<const Plan> get(const int32_t* lp, const int32_t* ls, int32_t num_seqs,
-                                  std::initializer_list<int32_t> options, Make&& make, Bytes&& bytes) {
+                                  std::initializer_list<int32_t> options, Make&& make, Bytes&& bytes,
+                                  const int32_t* more = nullptr) {
     const PlanEnv env = plan_env();
     const Tuning& t = env.tuning;
     key_.clear();
@@ -558,6 +559,7 @@ class LastPlan {
     key_.insert(key_.end(), {num_seqs, env.cus, env.xcds, t.kv_chunk_tiles, t.target_wgs, t.deal_rounds, t.suffix_weight});
     key_.insert(key_.end(), lp, lp + num_seqs);
     if (ls != nullptr) key_.insert(key_.end(), ls, ls + num_seqs);
+    if (more != nullptr) key_.insert(key_.end(), more, more + num_seqs);
     if (plan_ && key_ == kept_) return plan_;
     std::shared_ptr<const Plan> p = std::make_shared<const Plan>(make(env));
     if (bytes(*p) + key_.size() * sizeof(int32_t) <= kMaxKeptPlanBytes) {
@@ -722,6 +724,47 @@ std::shared_ptr<const StepPlan> diff_plan(const int32_t* lp, const int32_t* ls, 
     return make_step_plan(e, lp, ls, num_seqs, kinds);
   };
   return last.get(lp, ls, num_seqs, {num_pairs, gqa_group, head_dim, page_size, int32_t(kv_dtype)}, make, step_kept_bytes);
+}
+
+// The plan of a call with shaped scores: like a step's, over the keys that its window and prefix
+// masks leave.  Chunks run on 256-row tiles like the extend kernel's; a decode's chunks count
+// from shaped_decode_base, which its kernel adds again.
+std::shared_ptr<const StepPlan> shaped_plan(const int32_t* lp, const int32_t* ls, int32_t num_seqs, int32_t num_kv_heads,
+                                            int32_t gqa_group, int32_t head_dim, int32_t page_size, cw_kv_dtype_t kv_dtype,
+                                            int32_t window, const int32_t* full_lens) {
+  thread_local LastPlan<StepPlan> last;
+  auto make = [&](const PlanEnv& e) {
+    const bool fp8 = kv_dtype == CW_KV_FP8_E4M3FN;
+    const PlanKinds kinds{
+        [&](const PlanEnv& env, const int32_t* lp_e, const int32_t* ls_e, int32_t n, const int32_t* cu, const int32_t* bt) {
+          std::vector<int32_t> full;  // a prefix mask ends with its sequence
+          if (full_lens != nullptr)
+            for (int32_t b = 0; b < n; ++b) full.push_back(std::min(full_lens[bt[b]], lp_e[b] + ls_e[b]));
+          KeyLimits limits;
+          limits.window = window;
+          limits.full_lens = full_lens != nullptr ? full.data() : nullptr;
+          ExtendPlan plan = build_extend_plan(lp_e, ls_e, n, num_kv_heads, gqa_group, head_dim, LDS_BLOCK_M, 1, env.cus,
+                                              env.xcds, env.tuning, cu, bt, 1, 0, &limits);
+          if (full_lens != nullptr)
+            for (WorkItem& w : plan.items)
+              if (w.seq >= 0) w.pad = full[w.seq];
+          return plan;
+        },
+        [&](const PlanEnv& env, const int32_t* lp_d, int32_t n, size_t meta_at, const int32_t* cu, const int32_t* bt) {
+          const int32_t unit = std::max(shaped_decode_keys_per_tile(), page_size);
+          std::vector<int32_t> rest(lp_d, lp_d + n);
+          for (int32_t& x : rest) x -= shaped_decode_base(x, window, unit);
+          ExtendPlan plan = build_decode_plan(rest.data(), n, num_kv_heads, gqa_group, head_dim, page_size,
+                                              shaped_decode_keys_per_tile(), shaped_decode_waves_per_cu(head_dim, fp8),
+                                              env.cus, env.tuning, meta_at, cu, bt, 1, true);
+          for (int32_t b = 0; b < n; ++b) plan.seqs[b].lp = lp_d[b];
+          return plan;
+        }};
+    return make_step_plan(e, lp, ls, num_seqs, kinds);
+  };
+  return last.get(lp, ls, num_seqs,
+                  {num_kv_heads, gqa_group, head_dim, page_size, int32_t(kv_dtype), window, full_lens != nullptr ? 1 : 0}, make,
+                  step_kept_bytes, full_lens);
 }
 
 // Kernel arguments of a plan whose meta is read at `meta` and whose partials
@@ -1208,6 +1251,257 @@ cw_status_t diff_impl(const void* q, const void* k_new, const void* v_new, const
   }, arg_plan);
 }
 
+cw_status_t check_score_shape(float score_cap, int32_t window, const int32_t* full_lens, int32_t num_seqs) {
+  if (score_cap != 0.f && !(score_cap >= 0x1p-10f && score_cap <= 4096.f))
+    return fail(CW_ERR_UNSUPPORTED, "score_cap = %g (supported: 0, or 2^-10 .. 4096)", double(score_cap));
+  if (window < 0) return fail(CW_ERR_BAD_LENS, "window = %d is negative", window);
+  for (int32_t b = 0; full_lens != nullptr && b < num_seqs; ++b)
+    if (full_lens[b] < 0) return fail(CW_ERR_BAD_LENS, "sequence %d: prefix mask of %d tokens", b, full_lens[b]);
+  return CW_OK;
+}
+
+cw_status_t shaped_impl(const void* q, const void* k_new, const void* v_new, const void* k_pool, const void* v_pool,
+                        const float* k_scale, const float* v_scale, const int32_t* block_table, int32_t bt_stride,
+                        int32_t num_pages, const int32_t* lp, const int32_t* ls, int32_t num_seqs, int32_t num_kv_heads,
+                        int32_t gqa_group, int32_t head_dim, int32_t page_size, float softmax_scale,
+                        cw_kv_dtype_t kv_dtype, float score_cap, const float* slopes, int32_t window,
+                        const int32_t* key_begins, const int32_t* full_lens, void* out, float* lse, void* workspace,
+                        size_t workspace_bytes, hipStream_t stream) {
+  cw_status_t s = check_shape(num_seqs, num_kv_heads, gqa_group, head_dim, page_size);
+  if (s != CW_OK) return s;
+  s = check_dtype(kv_dtype, k_scale, v_scale);
+  if (s != CW_OK) return s;
+  if (!(softmax_scale > 0.0f) || !std::isfinite(softmax_scale))
+    return fail(CW_ERR_UNSUPPORTED, "softmax_scale = %g (must be finite and > 0)", double(softmax_scale));
+  if (num_pages < 0) return fail(CW_ERR_BAD_LENS, "num_pages = %d is negative", num_pages);
+  s = check_lens(lp, ls, num_seqs, bt_stride, page_size, num_kv_heads, gqa_group, head_dim, true);
+  if (s != CW_OK) return s;
+  s = check_score_shape(score_cap, window, full_lens, num_seqs);
+  if (s != CW_OK) return s;
+  const float log2e = 1.4426950408889634f;
+  const float factor = score_cap > 0.f ? softmax_scale / score_cap * (2.f * log2e) : softmax_scale * log2e;
+  if (!std::isfinite(factor)) return fail(CW_ERR_UNSUPPORTED, "softmax_scale = %g is too large", double(softmax_scale));
+  const int64_t total = sum_suffix(ls, num_seqs);
+  if (total == 0) return CW_OK;
+  if (!q || !k_new || !v_new || !out || !block_table)
+    return fail(CW_ERR_NULL, "q, k_new, v_new, out and block_table are required");
+  bool any_prefix = false;
+  for (int32_t b = 0; b < num_seqs; ++b) any_prefix |= lp[b] > 0 && ls[b] > 0;
+  if (any_prefix && (!k_pool || !v_pool)) return fail(CW_ERR_NULL, "k_pool / v_pool is NULL");
+  if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(out) || !aligned16(k_pool) ||
+      !aligned16(v_pool) || !aligned16(workspace))
+    return fail(CW_ERR_ALIGN, "tensor and workspace pointers must be 16-byte aligned");
+  if ((reinterpret_cast<uintptr_t>(block_table) | reinterpret_cast<uintptr_t>(slopes) |
+       reinterpret_cast<uintptr_t>(key_begins) | reinterpret_cast<uintptr_t>(lse) |
+       reinterpret_cast<uintptr_t>(k_scale) | reinterpret_cast<uintptr_t>(v_scale)) & 3u)
+    return fail(CW_ERR_ALIGN, "block_table, slopes, key_begins, lse and scales must be 4-byte aligned");
+
+  const std::shared_ptr<const StepPlan> kept = shaped_plan(lp, ls, num_seqs, num_kv_heads, gqa_group, head_dim, page_size,
+                                                           kv_dtype, window, full_lens);
+  const StepPlan& sp = *kept;
+  if (workspace == nullptr || workspace_bytes < sp.total_bytes)
+    return fail(CW_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", workspace_bytes, sp.total_bytes);
+  s = check_attention_alias(q, k_new, v_new, k_pool, v_pool, k_scale, v_scale, block_table, bt_stride, num_pages,
+                            num_seqs, num_kv_heads, gqa_group, head_dim, page_size, kv_dtype, total, out, lse,
+                            workspace, workspace_bytes);
+  if (s != CW_OK) return s;
+  const size_t hq = size_t(num_kv_heads) * gqa_group;
+  s = check_no_alias({{out, size_t(total) * hq * head_dim * 2, "out"}, {lse, size_t(total) * hq * 4, "lse"},
+                      {workspace, workspace_bytes, "workspace"}},
+                     {{slopes, hq * 4, "slopes"}, {key_begins, size_t(total) * 4, "key_begins"}});
+  if (s != CW_OK) return s;
+
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  auto params = [&](const ExtendPlan& plan, const uint8_t* meta, size_t part) {
+    ShapedParams p{};
+    p.a = plan_params(plan, meta, ws, part);
+    p.a.q = q;
+    p.a.k_new = k_new;
+    p.a.v_new = v_new;
+    p.a.k_pool = k_pool;
+    p.a.v_pool = v_pool;
+    p.a.k_scale = k_scale;
+    p.a.v_scale = v_scale;
+    p.a.block_table = block_table;
+    p.a.out = out;
+    p.a.lse = lse;
+    p.a.bt_stride = bt_stride;
+    p.a.num_kv_heads = num_kv_heads;
+    p.a.gqa_group = gqa_group;
+    p.a.num_seqs = num_seqs;
+    p.slopes = slopes;
+    p.begins = key_begins;
+    p.score_factor = factor;
+    p.cap2 = score_cap * log2e;
+    p.window = window;
+    p.page_shift = page_size == 16 ? 4 : 6;
+    return p;
+  };
+  const bool fp8 = kv_dtype == CW_KV_FP8_E4M3FN;
+  CompactUpload cu;
+  const bool compact = !sp.dec.empty() && compact_upload(sp.dec_plan, sp.off_dec_meta, &cu);
+  auto launch = [&](const uint8_t* meta, const ArgPlanBuf* ap) -> cw_status_t {
+    hipError_t e = hipSuccess;
+    if (!sp.dec.empty()) {
+      ShapedParams pd = params(sp.dec_plan, ap != nullptr ? nullptr : meta + sp.off_dec_meta, sp.off_dec_part);
+      if (ap != nullptr) {
+        pd.a.ap_seqs = static_cast<int32_t>(sp.off_dec_meta + sp.dec_plan.off_seqs);
+        pd.a.ap_desc = static_cast<int32_t>(cu.bytes);
+      }
+      if ((e = launch_shaped_decode(pd, head_dim, fp8, stream, ap)) != hipSuccess)
+        return hip_fail(e, "shaped decode kernel launch");
+      if ((e = launch_combine(pd.a, head_dim, sp.dec_plan.max_parts, stream, ap)) != hipSuccess)
+        return hip_fail(e, "combine kernel launch");
+    }
+    if (!sp.ext.empty()) {
+      ShapedParams pe = params(sp.ext_plan, ap != nullptr ? nullptr : meta + sp.off_ext_meta, sp.off_ext_part);
+      if (ap != nullptr) {
+        pe.a.ap_seqs = static_cast<int32_t>(sp.off_ext_meta + sp.ext_plan.off_seqs);
+        pe.a.ap_items = static_cast<int32_t>(sp.off_ext_meta + sp.ext_plan.off_items);
+        pe.a.ap_groups = static_cast<int32_t>(sp.off_ext_meta + sp.ext_plan.off_groups);
+      }
+      e = head_dim == 64 ? launch_shaped_extend_d64(pe, fp8, stream, ap) : launch_shaped_extend_d128(pe, fp8, stream, ap);
+      if (e != hipSuccess) return hip_fail(e, "shaped extend kernel launch");
+      if ((e = launch_combine(pe.a, head_dim, sp.ext_plan.max_parts, stream, ap)) != hipSuccess)
+        return hip_fail(e, "combine kernel launch");
+    }
+    return CW_OK;
+  };
+  auto head = [&](uint8_t* h) {
+    std::fill(h, h + sp.off_ext_meta, uint8_t(0));
+    if (!sp.ext.empty()) pack_plan_meta(sp.ext_plan, h + sp.off_ext_meta);
+  };
+  const bool arg_plan = arg_plans() && (sp.dec.empty() || (compact && compact_arg_fits(cu.bytes)));
+  const size_t whole_bytes = sp.off_ext_meta + sp.ext_plan.whole_meta_bytes + sp.dec_plan.whole_meta_bytes;
+  return stage_and_launch(sp.meta_bytes, whole_bytes, ws, stream, [&](uint8_t* h) {
+    head(h);
+    if (!sp.dec.empty()) pack_plan_meta(sp.dec_plan, h + sp.off_dec_meta);
+  }, launch, false, plan_direct(false), compact ? &cu : nullptr, [&](uint8_t* h) {
+    head(h);
+    pack_plan_head(sp.dec_plan, h + sp.off_dec_meta);
+  }, arg_plan);
+}
+
+// Norm, rotation and page write; num_axes 0: one position per token.
+cw_status_t norm_rope_impl(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                           int64_t v_stride, int32_t num_tokens, int32_t num_q_heads, int32_t num_kv_heads,
+                           int32_t head_dim, const float* q_weight, const float* k_weight, float eps,
+                           const float* cos_sin, int32_t num_positions, int32_t rotary_dim, int32_t interleaved,
+                           const int32_t* positions, int32_t num_axes, const int32_t* axis_of, void* q_out,
+                           void* k_out, void* v_out, void* k_pool, void* v_pool, const float* k_scale,
+                           const float* v_scale, const int64_t* slots, int32_t num_pages, int32_t page_size,
+                           cw_kv_dtype_t kv_dtype, hipStream_t stream) {
+  const bool pools = k_pool != nullptr || v_pool != nullptr;
+  cw_status_t s = check_shape(0, num_kv_heads, 1, head_dim, pools ? page_size : 16);
+  if (s != CW_OK) return s;
+  if (num_q_heads < 1 || num_q_heads > 16384)
+    return fail(CW_ERR_UNSUPPORTED, "num_q_heads = %d (supported: 1..16384)", num_q_heads);
+  if (rotary_dim < 16 || rotary_dim > head_dim || rotary_dim % 16 != 0)
+    return fail(CW_ERR_UNSUPPORTED, "rotary_dim = %d (supported: multiples of 16 in 16..head_dim)", rotary_dim);
+  if (!(eps >= 0.f) || !std::isfinite(eps))
+    return fail(CW_ERR_UNSUPPORTED, "eps = %g (must be finite and >= 0)", double(eps));
+  if (num_tokens < 0 || num_tokens > INT32_MAX / 32 || num_positions < 0 || num_pages < 0)
+    return fail(CW_ERR_BAD_LENS, "count out of range (num_tokens = %d, num_positions = %d, num_pages = %d)", num_tokens,
+                num_positions, num_pages);
+  if (pools) {
+    s = check_dtype(kv_dtype, k_scale, v_scale);
+    if (s != CW_OK) return s;
+  }
+  if (num_axes > 0) {
+    if (num_axes > 4) return fail(CW_ERR_UNSUPPORTED, "num_axes = %d (supported: 1..4)", num_axes);
+    if (axis_of == nullptr) return fail(CW_ERR_NULL, "axis_of_h is NULL");
+    for (int32_t i = 0; i < rotary_dim / 2; ++i)
+      if (axis_of[i] < 0 || axis_of[i] >= num_axes)
+        return fail(CW_ERR_UNSUPPORTED, "axis_of_h[%d] = %d with num_axes = %d", i, axis_of[i], num_axes);
+  }
+  if (num_tokens == 0) return CW_OK;
+  if (!q || !k || !q_out || !k_out || !cos_sin || !positions)
+    return fail(CW_ERR_NULL, "q, k, q_out, k_out, cos_sin and positions are required");
+  if (pools && (!k_pool || !v_pool || !slots || !v))
+    return fail(CW_ERR_NULL, "a page write needs k_pool, v_pool, slots and v");
+  if (v_out && !v) return fail(CW_ERR_NULL, "v_out without v");
+  const int64_t q_row = int64_t(num_q_heads) * head_dim, kv_row = int64_t(num_kv_heads) * head_dim;
+  auto bad_stride = [&](const void* x, int64_t stride, int64_t row) {
+    return x != nullptr && (stride % 8 != 0 || (num_tokens > 1 && stride < row) || stride > (int64_t(1) << 31));
+  };
+  if (bad_stride(q, q_stride, q_row) || bad_stride(k, k_stride, kv_row) || bad_stride(v, v_stride, kv_row))
+    return fail(CW_ERR_ALIGN, "token strides must be multiples of 8 elements and hold a token's heads");
+  for (const void* x : {q, k, v, static_cast<const void*>(q_weight), static_cast<const void*>(k_weight),
+                        static_cast<const void*>(cos_sin), static_cast<const void*>(q_out),
+                        static_cast<const void*>(k_out), static_cast<const void*>(v_out),
+                        static_cast<const void*>(k_pool), static_cast<const void*>(v_pool)})
+    if (!aligned16(x)) return fail(CW_ERR_ALIGN, "tensor pointers must be 16-byte aligned");
+  if ((reinterpret_cast<uintptr_t>(positions) & 3u) || (reinterpret_cast<uintptr_t>(slots) & 7u) ||
+      ((reinterpret_cast<uintptr_t>(k_scale) | reinterpret_cast<uintptr_t>(v_scale)) & 3u))
+    return fail(CW_ERR_ALIGN, "positions must be 4-byte, slots 8-byte and scales 4-byte aligned");
+  // an output may be its own contiguous input; the inputs between the first and the last
+  // token's heads may hold other columns of a projection's output
+  auto span_in = [&](const void* x, int64_t stride, int64_t row) {
+    return (size_t(num_tokens - 1) * size_t(num_tokens > 1 ? stride : 0) + size_t(row)) * 2;
+  };
+  auto in_place = [&](const void* x, int64_t stride, int64_t row, const void* y) {
+    return x == y && (stride == row || num_tokens == 1);
+  };
+  const bool fp8 = pools && kv_dtype == CW_KV_FP8_E4M3FN;
+  const size_t out_q = size_t(num_tokens) * q_row * 2, out_kv = size_t(num_tokens) * kv_row * 2;
+  const size_t pool = pools ? size_t(num_pages) * kv_row * page_size * (fp8 ? 1 : 2) : 0;
+  const size_t scales = fp8 ? size_t(num_pages) * num_kv_heads * 4 : 0;
+  s = check_no_alias(
+      {{q_out, out_q, "q_out"}, {k_out, out_kv, "k_out"}, {v_out, out_kv, "v_out"}, {k_pool, pool, "k_pool"},
+       {v_pool, pool, "v_pool"}},
+      {{q_weight, size_t(head_dim) * 4, "q_weight"}, {k_weight, size_t(head_dim) * 4, "k_weight"},
+       {cos_sin, size_t(num_positions) * rotary_dim * 4, "cos_sin"}, {positions, size_t(num_tokens) * std::max(1, num_axes) * 4, "positions"},
+       {slots, pools ? size_t(num_tokens) * 8 : 0, "slots"}, {k_scale, scales, "k_scale"}, {v_scale, scales, "v_scale"}});
+  if (s != CW_OK) return s;
+  const Span in_q{q, span_in(q, q_stride, q_row), "q"}, in_k{k, span_in(k, k_stride, kv_row), "k"},
+      in_v{v, v ? span_in(v, v_stride, kv_row) : 0, "v"};
+  struct Out {
+    Span span;
+    const Span* own;  // the input that it may be, and whether it is
+    bool same;
+  };
+  const Out outs[] = {{{q_out, out_q, "q_out"}, &in_q, in_place(q, q_stride, q_row, q_out)},
+                      {{k_out, out_kv, "k_out"}, &in_k, in_place(k, k_stride, kv_row, k_out)},
+                      {{v_out, out_kv, "v_out"}, &in_v, in_place(v, v_stride, kv_row, v_out)},
+                      {{k_pool, pool, "k_pool"}, nullptr, false},
+                      {{v_pool, pool, "v_pool"}, nullptr, false}};
+  for (const Out& o : outs)
+    for (const Span* i : {&in_q, &in_k, &in_v})
+      if (!(o.same && i == o.own) && overlap(o.span, *i))
+        return fail(CW_ERR_ALIAS, "%s overlaps %s", o.span.name, i->name);
+  NormRopeParams p{};
+  p.q = q;
+  p.k = k;
+  p.v = v_out || pools ? v : nullptr;
+  p.q_weight = q_weight;
+  p.k_weight = k_weight;
+  p.cos_sin = cos_sin;
+  p.positions = positions;
+  p.slots = slots;
+  p.q_out = q_out;
+  p.k_out = k_out;
+  p.v_out = v_out;
+  p.k_pool = k_pool;
+  p.v_pool = v_pool;
+  p.k_scale = k_scale;
+  p.v_scale = v_scale;
+  p.q_stride = q_stride;
+  p.k_stride = k_stride;
+  p.v_stride = v_stride;
+  p.eps = eps;
+  p.num_tokens = num_tokens;
+  p.hq = num_q_heads;
+  p.hkv = num_kv_heads;
+  p.num_positions = num_positions;
+  p.rot = rotary_dim;
+  p.num_pages = num_pages;
+  p.page_size = page_size;
+  p.num_axes = num_axes;
+  for (int32_t i = 0; num_axes > 0 && i < rotary_dim / 2; ++i) p.axis_of[i / 16] |= uint32_t(axis_of[i]) << (2 * (i % 16));
+  const hipError_t e = launch_qk_norm_rope(p, head_dim, interleaved != 0, !pools ? 0 : fp8 ? 2 : 1, stream);
+  return e == hipSuccess ? CW_OK : hip_fail(e, "qk_norm_rope kernel launch");
+}
+
 // Runs an entry point's body: a failed host allocation (or any other C++
 // exception) becomes a status, so nothing is thrown across the C ABI.
 template <class F>
@@ -1441,106 +1735,109 @@ cw_status_t cw_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int6
                             int32_t num_pages, int32_t page_size, cw_kv_dtype_t kv_dtype,
                             hipStream_t stream) {
   return guarded([&]() -> cw_status_t {
-    const bool pools = k_pool != nullptr || v_pool != nullptr;
-    cw_status_t s = check_shape(0, num_kv_heads, 1, head_dim, pools ? page_size : 16);
-    if (s != CW_OK) return s;
-    if (num_q_heads < 1 || num_q_heads > 16384)
-      return fail(CW_ERR_UNSUPPORTED, "num_q_heads = %d (supported: 1..16384)", num_q_heads);
-    if (rotary_dim < 16 || rotary_dim > head_dim || rotary_dim % 16 != 0)
-      return fail(CW_ERR_UNSUPPORTED, "rotary_dim = %d (supported: multiples of 16 in 16..head_dim)", rotary_dim);
-    if (!(eps >= 0.f) || !std::isfinite(eps))
-      return fail(CW_ERR_UNSUPPORTED, "eps = %g (must be finite and >= 0)", double(eps));
-    if (num_tokens < 0 || num_tokens > INT32_MAX / 32 || num_positions < 0 || num_pages < 0)
-      return fail(CW_ERR_BAD_LENS, "count out of range (num_tokens = %d, num_positions = %d, num_pages = %d)", num_tokens,
-                  num_positions, num_pages);
-    if (pools) {
-      s = check_dtype(kv_dtype, k_scale, v_scale);
-      if (s != CW_OK) return s;
-    }
+    return norm_rope_impl(q, q_stride, k, k_stride, v, v_stride, num_tokens, num_q_heads, num_kv_heads, head_dim,
+                          q_weight, k_weight, eps, cos_sin, num_positions, rotary_dim, interleaved, positions, 0,
+                          nullptr, q_out, k_out, v_out, k_pool, v_pool, k_scale, v_scale, slots, num_pages,
+                          page_size, kv_dtype, stream);
+  });
+}
+
+cw_status_t cw_qk_norm_rope_axes(const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                                 const void* v, int64_t v_stride, int32_t num_tokens,
+                                 int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                                 const float* q_weight, const float* k_weight, float eps,
+                                 const float* cos_sin, int32_t num_positions, int32_t rotary_dim,
+                                 int32_t interleaved, const int32_t* positions, int32_t num_axes,
+                                 const int32_t* axis_of_h, void* q_out, void* k_out, void* v_out,
+                                 void* k_pool, void* v_pool, const float* k_scale,
+                                 const float* v_scale, const int64_t* slots, int32_t num_pages,
+                                 int32_t page_size, cw_kv_dtype_t kv_dtype, hipStream_t stream) {
+  return guarded([&]() -> cw_status_t {
+    if (num_axes < 1) return fail(CW_ERR_UNSUPPORTED, "num_axes = %d (supported: 1..4)", num_axes);
+    return norm_rope_impl(q, q_stride, k, k_stride, v, v_stride, num_tokens, num_q_heads, num_kv_heads, head_dim,
+                          q_weight, k_weight, eps, cos_sin, num_positions, rotary_dim, interleaved, positions,
+                          num_axes, axis_of_h, q_out, k_out, v_out, k_pool, v_pool, k_scale, v_scale, slots,
+                          num_pages, page_size, kv_dtype, stream);
+  });
+}
+
+cw_status_t cw_residual_norm(const void* x, int64_t x_stride, const void* residual, int32_t residual_fp32,
+                             int32_t num_tokens, int32_t width, const float* post_weight, const void* gate,
+                             int64_t gate_stride, float residual_scale, const float* pre_weight, float eps,
+                             void* residual_out, void* y_out, hipStream_t stream) {
+  return guarded([&]() -> cw_status_t {
+    if (width < 8 || width > kResidualMaxWidth || width % 8 != 0)
+      return fail(CW_ERR_UNSUPPORTED, "width = %d (supported: multiples of 8 in 8..%d)", width, kResidualMaxWidth);
+    if (!(eps >= 0.f) || !std::isfinite(eps) || !std::isfinite(residual_scale))
+      return fail(CW_ERR_UNSUPPORTED, "eps = %g, residual_scale = %g (must be finite, eps >= 0)", double(eps),
+                  double(residual_scale));
+    if (num_tokens < 0 || num_tokens > INT32_MAX / 32) return fail(CW_ERR_BAD_LENS, "num_tokens = %d out of range", num_tokens);
     if (num_tokens == 0) return CW_OK;
-    if (!q || !k || !q_out || !k_out || !cos_sin || !positions)
-      return fail(CW_ERR_NULL, "q, k, q_out, k_out, cos_sin and positions are required");
-    if (pools && (!k_pool || !v_pool || !slots || !v))
-      return fail(CW_ERR_NULL, "a page write needs k_pool, v_pool, slots and v");
-    if (v_out && !v) return fail(CW_ERR_NULL, "v_out without v");
-    const int64_t q_row = int64_t(num_q_heads) * head_dim, kv_row = int64_t(num_kv_heads) * head_dim;
-    auto bad_stride = [&](const void* x, int64_t stride, int64_t row) {
-      return x != nullptr && (stride % 8 != 0 || (num_tokens > 1 && stride < row) || stride > (int64_t(1) << 31));
-    };
-    if (bad_stride(q, q_stride, q_row) || bad_stride(k, k_stride, kv_row) || bad_stride(v, v_stride, kv_row))
-      return fail(CW_ERR_ALIGN, "token strides must be multiples of 8 elements and hold a token's heads");
-    for (const void* x : {q, k, v, static_cast<const void*>(q_weight), static_cast<const void*>(k_weight),
-                          static_cast<const void*>(cos_sin), static_cast<const void*>(q_out),
-                          static_cast<const void*>(k_out), static_cast<const void*>(v_out),
-                          static_cast<const void*>(k_pool), static_cast<const void*>(v_pool)})
-      if (!aligned16(x)) return fail(CW_ERR_ALIGN, "tensor pointers must be 16-byte aligned");
-    if ((reinterpret_cast<uintptr_t>(positions) & 3u) || (reinterpret_cast<uintptr_t>(slots) & 7u) ||
-        ((reinterpret_cast<uintptr_t>(k_scale) | reinterpret_cast<uintptr_t>(v_scale)) & 3u))
-      return fail(CW_ERR_ALIGN, "positions must be 4-byte, slots 8-byte and scales 4-byte aligned");
-    // an output may be its own contiguous input; the inputs between the first and the last
-    // token's heads may hold other columns of a projection's output
-    auto span_in = [&](const void* x, int64_t stride, int64_t row) {
-      return (size_t(num_tokens - 1) * size_t(num_tokens > 1 ? stride : 0) + size_t(row)) * 2;
-    };
-    auto in_place = [&](const void* x, int64_t stride, int64_t row, const void* y) {
-      return x == y && (stride == row || num_tokens == 1);
-    };
-    const bool fp8 = pools && kv_dtype == CW_KV_FP8_E4M3FN;
-    const size_t out_q = size_t(num_tokens) * q_row * 2, out_kv = size_t(num_tokens) * kv_row * 2;
-    const size_t pool = pools ? size_t(num_pages) * kv_row * page_size * (fp8 ? 1 : 2) : 0;
-    const size_t scales = fp8 ? size_t(num_pages) * num_kv_heads * 4 : 0;
-    s = check_no_alias(
-        {{q_out, out_q, "q_out"}, {k_out, out_kv, "k_out"}, {v_out, out_kv, "v_out"}, {k_pool, pool, "k_pool"},
-         {v_pool, pool, "v_pool"}},
-        {{q_weight, size_t(head_dim) * 4, "q_weight"}, {k_weight, size_t(head_dim) * 4, "k_weight"},
-         {cos_sin, size_t(num_positions) * rotary_dim * 4, "cos_sin"}, {positions, size_t(num_tokens) * 4, "positions"},
-         {slots, pools ? size_t(num_tokens) * 8 : 0, "slots"}, {k_scale, scales, "k_scale"}, {v_scale, scales, "v_scale"}});
+    if (!x || !residual || !residual_out) return fail(CW_ERR_NULL, "x, residual and residual_out are required");
+    if ((pre_weight == nullptr) != (y_out == nullptr)) return fail(CW_ERR_NULL, "pre_weight and y_out go together");
+    const bool many = num_tokens > 1;
+    auto bad_stride = [&](int64_t stride) { return stride % 8 != 0 || (many && stride < width) || stride > (int64_t(1) << 31); };
+    if (bad_stride(x_stride) || (gate && gate_stride != 0 && bad_stride(gate_stride)))
+      return fail(CW_ERR_ALIGN, "token strides must be multiples of 8 elements and hold a token's row");
+    for (const void* t : {x, residual, static_cast<const void*>(post_weight), gate, static_cast<const void*>(pre_weight),
+                          static_cast<const void*>(residual_out), static_cast<const void*>(y_out)})
+      if (!aligned16(t)) return fail(CW_ERR_ALIGN, "tensor pointers must be 16-byte aligned");
+    auto span = [&](int64_t stride) { return (size_t(num_tokens - 1) * size_t(many ? stride : 0) + size_t(width)) * 2; };
+    const size_t rows = size_t(num_tokens) * width, stream_bytes = rows * (residual_fp32 ? 4 : 2);
+    const cw_status_t s = check_no_alias(
+        {{residual_out, stream_bytes, "residual_out"}, {y_out, rows * 2, "y_out"}},
+        {{x, span(x_stride), "x"}, {post_weight, size_t(width) * 4, "post_weight"}, {pre_weight, size_t(width) * 4, "pre_weight"},
+         {gate, span(gate_stride), "gate"}, {residual == residual_out ? nullptr : residual, stream_bytes, "residual"}});
     if (s != CW_OK) return s;
-    const Span in_q{q, span_in(q, q_stride, q_row), "q"}, in_k{k, span_in(k, k_stride, kv_row), "k"},
-        in_v{v, v ? span_in(v, v_stride, kv_row) : 0, "v"};
-    struct Out {
-      Span span;
-      const Span* own;  // the input that it may be, and whether it is
-      bool same;
-    };
-    const Out outs[] = {{{q_out, out_q, "q_out"}, &in_q, in_place(q, q_stride, q_row, q_out)},
-                        {{k_out, out_kv, "k_out"}, &in_k, in_place(k, k_stride, kv_row, k_out)},
-                        {{v_out, out_kv, "v_out"}, &in_v, in_place(v, v_stride, kv_row, v_out)},
-                        {{k_pool, pool, "k_pool"}, nullptr, false},
-                        {{v_pool, pool, "v_pool"}, nullptr, false}};
-    for (const Out& o : outs)
-      for (const Span* i : {&in_q, &in_k, &in_v})
-        if (!(o.same && i == o.own) && overlap(o.span, *i))
-          return fail(CW_ERR_ALIAS, "%s overlaps %s", o.span.name, i->name);
-    NormRopeParams p{};
-    p.q = q;
-    p.k = k;
-    p.v = v_out || pools ? v : nullptr;
-    p.q_weight = q_weight;
-    p.k_weight = k_weight;
-    p.cos_sin = cos_sin;
-    p.positions = positions;
-    p.slots = slots;
-    p.q_out = q_out;
-    p.k_out = k_out;
-    p.v_out = v_out;
-    p.k_pool = k_pool;
-    p.v_pool = v_pool;
-    p.k_scale = k_scale;
-    p.v_scale = v_scale;
-    p.q_stride = q_stride;
-    p.k_stride = k_stride;
-    p.v_stride = v_stride;
+    if (y_out && overlap({y_out, rows * 2, "y_out"}, {residual, stream_bytes, "residual"}))
+      return fail(CW_ERR_ALIAS, "y_out overlaps residual");
+    ResidualNormParams p{};
+    p.x = x;
+    p.residual = residual;
+    p.post_weight = post_weight;
+    p.gate = gate;
+    p.pre_weight = pre_weight;
+    p.residual_out = residual_out;
+    p.y_out = y_out;
+    p.x_stride = x_stride;
+    p.gate_stride = gate ? gate_stride : 0;
+    p.scale = residual_scale;
     p.eps = eps;
     p.num_tokens = num_tokens;
-    p.hq = num_q_heads;
-    p.hkv = num_kv_heads;
-    p.num_positions = num_positions;
-    p.rot = rotary_dim;
-    p.num_pages = num_pages;
-    p.page_size = page_size;
-    const hipError_t e = launch_qk_norm_rope(p, head_dim, interleaved != 0, !pools ? 0 : fp8 ? 2 : 1, stream);
-    return e == hipSuccess ? CW_OK : hip_fail(e, "qk_norm_rope kernel launch");
+    p.width = width;
+    const hipError_t e = launch_residual_norm(p, residual_fp32 != 0, stream);
+    return e == hipSuccess ? CW_OK : hip_fail(e, "residual_norm kernel launch");
+  });
+}
+
+size_t cw_shaped_workspace_bytes(const int32_t* prefix_lens_h, const int32_t* suffix_lens_h, int32_t num_seqs,
+                                 int32_t num_kv_heads, int32_t gqa_group, int32_t head_dim, int32_t page_size,
+                                 cw_kv_dtype_t kv_dtype, int32_t window, const int32_t* full_lens_h) {
+  return guarded_value<size_t>(0, [&]() -> size_t {
+    if (check_shape(num_seqs, num_kv_heads, gqa_group, head_dim, page_size) != CW_OK) return 0;
+    if (kv_dtype != CW_KV_BF16 && kv_dtype != CW_KV_FP8_E4M3FN) return 0;
+    if (check_lens(prefix_lens_h, suffix_lens_h, num_seqs, 0, page_size, num_kv_heads, gqa_group, head_dim, false) != CW_OK)
+      return 0;
+    if (check_score_shape(0.f, window, full_lens_h, num_seqs) != CW_OK) return 0;
+    return shaped_plan(prefix_lens_h, suffix_lens_h, num_seqs, num_kv_heads, gqa_group, head_dim, page_size, kv_dtype, window,
+                       full_lens_h)
+        ->total_bytes;
+  });
+}
+
+cw_status_t cw_shaped_attention(const void* q, const void* k_new, const void* v_new, const void* k_pool,
+                                const void* v_pool, const float* k_scale, const float* v_scale,
+                                const int32_t* block_table, int32_t bt_stride, int32_t num_pages,
+                                const int32_t* prefix_lens_h, const int32_t* suffix_lens_h, int32_t num_seqs,
+                                int32_t num_kv_heads, int32_t gqa_group, int32_t head_dim, int32_t page_size,
+                                float softmax_scale, cw_kv_dtype_t kv_dtype, float score_cap, const float* slopes,
+                                int32_t window, const int32_t* key_begins, const int32_t* full_lens_h, void* out,
+                                float* lse, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  return guarded([&]() -> cw_status_t {
+    return shaped_impl(q, k_new, v_new, k_pool, v_pool, k_scale, v_scale, block_table, bt_stride, num_pages,
+                       prefix_lens_h, suffix_lens_h, num_seqs, num_kv_heads, gqa_group, head_dim, page_size,
+                       softmax_scale, kv_dtype, score_cap, slopes, window, key_begins, full_lens_h, out, lse, workspace,
+                       workspace_bytes, stream);
   });
 }
 

@@ -152,6 +152,24 @@ struct DiffParams {
 };
 constexpr int DIFF_BLOCK_M = 128;  // packed query rows of a diff extend work item
 
+// Attention with shaped scores: `a` as for the extend and decode kernels; a work item of a
+// chunk carries its sequence's prefix mask (tokens that see each other) in `pad`, and a decode
+// item's keys count from shaped_decode_base.
+struct ShapedParams {
+  ExtendParams a;
+  const float* slopes;    // [query heads] or nullptr: no bias
+  const int32_t* begins;  // [T] first visible position of each new token, or nullptr: 0
+  float score_factor;     // of a score q k: softmax_scale log2 e, with a cap times 2 / cap
+  float cap2;             // cap log2 e; 0: no cap
+  int32_t window;         // keys j > p - window are visible; 0: all
+  int32_t page_shift;     // log2 of the page size
+};
+// The key at which the decode chunks of a token at position lp start: all keys before it lie
+// before the window.  A multiple of `unit` (whole tiles and pages).
+__host__ __device__ inline int32_t shaped_decode_base(int32_t lp, int32_t window, int32_t unit) {
+  return window > 0 && lp + 1 > window ? (lp + 1 - window) / unit * unit : 0;
+}
+
 // Whole-block copies between two block pools (device page pool <-> host block
 // pool): block src_ids[i] of (src_k, src_v) goes to block dst_ids[i] of
 // (dst_k, dst_v); scales (fp8 pools) likewise, `scales_per_block` floats each.
@@ -218,6 +236,27 @@ struct NormRopeParams {
   int32_t num_pages;
   int32_t page_size;
   int32_t splits;  // waves per token
+  // with several position axes: positions of axis a at positions + a * num_tokens, and the axis
+  // of rotated pair i in bits 2 i, 2 i + 1 of axis_of
+  int32_t num_axes;  // 0: one axis
+  uint32_t axis_of[4];
+};
+
+// Norms around the residual stream (residual_norm.hip).
+constexpr int32_t kResidualMaxWidth = 16384;
+struct ResidualNormParams {
+  const void* x;             // bf16 [T, width], x_stride apart
+  const void* residual;      // bf16 or fp32 [T, width]
+  const float* post_weight;  // [width] or nullptr: x is not normed
+  const void* gate;          // bf16 [width] (gate_stride 0) or [T, width], or nullptr
+  const float* pre_weight;   // [width] or nullptr: no y
+  void* residual_out;
+  void* y_out;
+  int64_t x_stride, gate_stride;
+  float scale;
+  float eps;
+  int32_t num_tokens;
+  int32_t width;
 };
 
 // Sets the thread-local message returned by cw_last_error_message.
@@ -258,9 +297,15 @@ int diff_decode_keys_per_tile();
 int diff_decode_waves_per_cu(int head_dim, bool fp8);
 hipError_t launch_diff_combine(const DiffParams& p, int head_dim, int max_parts, hipStream_t stream,
                                const ArgPlanBuf* ap = nullptr);
+hipError_t launch_shaped_extend_d64(const ShapedParams& p, bool fp8, hipStream_t stream, const ArgPlanBuf* ap);
+hipError_t launch_shaped_extend_d128(const ShapedParams& p, bool fp8, hipStream_t stream, const ArgPlanBuf* ap);
+hipError_t launch_shaped_decode(const ShapedParams& p, int head_dim, bool fp8, hipStream_t stream, const ArgPlanBuf* ap);
+int shaped_decode_keys_per_tile();
+int shaped_decode_waves_per_cu(int head_dim, bool fp8);
 hipError_t launch_step_tables(const StepTablesParams& p, hipStream_t stream);
 // pool: 0 no page write, 1 bf16 pools, 2 fp8 pools
 hipError_t launch_qk_norm_rope(NormRopeParams p, int head_dim, bool interleaved, int pool, hipStream_t stream);
+hipError_t launch_residual_norm(const ResidualNormParams& p, bool wide, hipStream_t stream);
 hipError_t launch_check_table(const int32_t* bt, int32_t bt_stride, int32_t num_pages,
                               const SeqInfo* seqs, int32_t num_seqs, int32_t page_size,
                               int32_t* bad, hipStream_t stream);

@@ -85,7 +85,7 @@ __global__ __launch_bounds__(256) void combine_few_kernel(ExtendParams p, PlanAr
   const int G = p.gqa_group, hq = p.num_kv_heads * G;
   const int r = cg.q_row0 + lr;
   const int t = r / G, g = r - t * G;
-  const float inv = 1.f / L;
+  const float inv = L == 0.f ? 0.f : 1.f / L;  // (a row that no key is visible to: 0)
   uint16_t* orow = static_cast<uint16_t*>(p.out) + (size_t(sq.cu + t) * hq + size_t(cg.kvh) * G + g) * D + d0;
 #pragma unroll
   for (int e = 0; e < PER; ++e) orow[e] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(acc[e] * inv));
@@ -167,7 +167,7 @@ __global__ __launch_bounds__(256) void combine_many_kernel(ExtendParams p, PlanA
   const int r = cg.q_row0 + lr;
   const int t = r / G, g = r - t * G;
   const size_t row = size_t(sq.cu + t) * hq + size_t(cg.kvh) * G + g;
-  static_cast<uint16_t*>(p.out)[row * D + d] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(out / Lt));
+  static_cast<uint16_t*>(p.out)[row * D + d] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(Lt == 0.f ? 0.f : out / Lt));
   if (p.lse != nullptr && d == 0) p.lse[row] = (mstar + log2f(Lt)) * kLn2;
 }
 

@@ -48,8 +48,9 @@ __device__ __forceinline__ void load8(float (&f)[8], const float* src) {
   }
 }
 
-// POOL: 0 no page write, 1 bf16 pools, 2 fp8 pools.
-template <int D, bool INTER, int POOL>
+// POOL: 0 no page write, 1 bf16 pools, 2 fp8 pools.  AXES: a token has a position for each of
+// several axes, and each rotated pair follows one of them.
+template <int D, bool INTER, int POOL, bool AXES>
 __global__ __launch_bounds__(kThreads) void qk_norm_rope_kernel(NormRopeParams p) {
   constexpr int CH = D / 8;        // lanes per head
   constexpr int RPW = 64 / CH;     // heads per wave and step
@@ -60,7 +61,16 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_kernel(NormRopeParams p
   const int tok = item / p.splits;
   if (tok >= p.num_tokens) return;
   const int pos = p.positions[tok];
-  if (pos < 0 || pos >= p.num_positions) return;  // a padding token: nothing of it is written
+  bool outside = pos < 0 || pos >= p.num_positions;
+  int axis_pos[4] = {pos, pos, pos, pos};
+  if constexpr (AXES) {
+#pragma unroll
+    for (int a = 1; a < 4; ++a) {
+      if (a < p.num_axes) axis_pos[a] = p.positions[int64_t(a) * p.num_tokens + tok];
+      outside |= axis_pos[a] < 0 || axis_pos[a] >= p.num_positions;
+    }
+  }
+  if (outside) return;  // a padding token: nothing of it is written
   const int heads = p.hq + p.hkv + (p.v != nullptr ? p.hkv : 0);
   const int steps = (heads + RPW - 1) / RPW;
   const int per = (steps + p.splits - 1) / p.splits;
@@ -80,7 +90,46 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_kernel(NormRopeParams p
   }
   if (turns) {
     const float* row = p.cos_sin + size_t(pos) * p.rot;
-    if constexpr (INTER) {
+    if constexpr (AXES) {
+      // the axes of this lane's pairs (four or eight in a row), two bits each; pairs of one
+      // axis are read together
+      constexpr int PAIRS = INTER ? 4 : 8;
+      const bool first = INTER || 8 * c < half;
+      const int at = INTER ? 4 * c : first ? 8 * c : 8 * c - half;
+      const uint32_t word = at < 16 ? p.axis_of[0] : at < 32 ? p.axis_of[1] : at < 48 ? p.axis_of[2] : p.axis_of[3];
+      const uint32_t axes = word >> (2 * (at % 16)) & ((1u << (2 * PAIRS)) - 1);
+      auto row_of = [&](uint32_t a) {
+        const int at_pos = a == 0 ? axis_pos[0] : a == 1 ? axis_pos[1] : a == 2 ? axis_pos[2] : axis_pos[3];
+        return p.cos_sin + size_t(at_pos) * p.rot;
+      };
+      float cv[8], sv[8];
+      if (axes == (axes & 3) * (0x5555u & ((1u << (2 * PAIRS)) - 1))) {
+        const float* src = row_of(axes & 3);
+#pragma unroll
+        for (int e = 0; e < PAIRS; e += 4) {
+          const f32x4 a = *reinterpret_cast<const f32x4*>(src + at + e), b = *reinterpret_cast<const f32x4*>(src + half + at + e);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            cv[e + i] = a[i];
+            sv[e + i] = b[i];
+          }
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < PAIRS; ++e) {
+          const float* src = row_of(axes >> (2 * e) & 3);
+          cv[e] = src[at + e];
+          sv[e] = src[half + at + e];
+        }
+      }
+      if constexpr (!INTER) partner = first ? c + half / 8 : c - half / 8;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        cs[e] = cv[INTER ? e / 2 : e];
+        const float s = sv[INTER ? e / 2 : e];
+        sn[e] = (INTER ? e % 2 != 0 : !first) ? s : -s;
+      }
+    } else if constexpr (INTER) {
       const f32x4 a = *reinterpret_cast<const f32x4*>(row + 4 * c), b = *reinterpret_cast<const f32x4*>(row + half + 4 * c);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -190,14 +239,14 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_kernel(NormRopeParams p
   }
 }
 
-template <int D, bool INTER>
+template <int D, bool INTER, bool AXES>
 hipError_t launch_t(const NormRopeParams& p, int pool, hipStream_t stream) {
   constexpr int kWaves = kThreads / 64;
   const int64_t items = int64_t(p.num_tokens) * p.splits;
   const dim3 grid(static_cast<unsigned>((items + kWaves - 1) / kWaves));
-  if (pool == 0) hipLaunchKernelGGL((qk_norm_rope_kernel<D, INTER, 0>), grid, dim3(kThreads), 0, stream, p);
-  else if (pool == 1) hipLaunchKernelGGL((qk_norm_rope_kernel<D, INTER, 1>), grid, dim3(kThreads), 0, stream, p);
-  else hipLaunchKernelGGL((qk_norm_rope_kernel<D, INTER, 2>), grid, dim3(kThreads), 0, stream, p);
+  if (pool == 0) hipLaunchKernelGGL((qk_norm_rope_kernel<D, INTER, 0, AXES>), grid, dim3(kThreads), 0, stream, p);
+  else if (pool == 1) hipLaunchKernelGGL((qk_norm_rope_kernel<D, INTER, 1, AXES>), grid, dim3(kThreads), 0, stream, p);
+  else hipLaunchKernelGGL((qk_norm_rope_kernel<D, INTER, 2, AXES>), grid, dim3(kThreads), 0, stream, p);
   return hipGetLastError();
 }
 
@@ -212,8 +261,14 @@ hipError_t launch_qk_norm_rope(NormRopeParams p, int head_dim, bool interleaved,
   const int rpw = 64 / (head_dim / 8);
   const int steps = (p.hq + p.hkv + (p.v != nullptr ? p.hkv : 0) + rpw - 1) / rpw;
   p.splits = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(steps, kSplitWaves / p.num_tokens)));
-  if (head_dim == 64) return interleaved ? launch_t<64, true>(p, pool, stream) : launch_t<64, false>(p, pool, stream);
-  if (head_dim == 128) return interleaved ? launch_t<128, true>(p, pool, stream) : launch_t<128, false>(p, pool, stream);
+#define CW_CASE(D_, AXES_) \
+  if (head_dim == D_ && (p.num_axes > 0) == AXES_) \
+    return interleaved ? launch_t<D_, true, AXES_>(p, pool, stream) : launch_t<D_, false, AXES_>(p, pool, stream);
+  CW_CASE(64, false)
+  CW_CASE(128, false)
+  CW_CASE(64, true)
+  CW_CASE(128, true)
+#undef CW_CASE
   return hipErrorInvalidValue;
 }
 

@@ -1,0 +1,10 @@
+// Attention with shaped scores for chunks of new tokens: the instances for head dim 64.
+#include "shaped_extend.h"
+
+namespace cw {
+
+hipError_t launch_shaped_extend_d64(const ShapedParams& p, bool fp8, hipStream_t stream, const ArgPlanBuf* ap) {
+  return shaped::launch_extend_d<64>(p, fp8, stream, ap);
+}
+
+}  // namespace cw

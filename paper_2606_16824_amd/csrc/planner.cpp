@@ -35,6 +35,7 @@ size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 struct Tile {
   int32_t seq, kvh, q_row0, rows, kv_len, n_kt, n_pre;  // n_pre: key tiles wholly in the prefix
   int64_t rate;                                         // cost of a prefix key tile
+  int32_t k0;                                           // its first key tile (of n_kt)
 };
 
 // Work of one (sequence, kv head), or a share of it: items [first, first + n) of
@@ -117,7 +118,7 @@ int64_t span_cost(const Tile& t, int64_t a, int64_t b, int64_t suffix_weight) {
   return (pre * 100 + suf * suffix_weight) * t.rate / 100;
 }
 int64_t tile_cost(const Costs& c, const Tile& t, int64_t suffix_weight) {
-  return c.item + span_cost(t, 0, t.n_kt, suffix_weight);
+  return c.item + span_cost(t, t.k0, t.n_kt, suffix_weight);
 }
 // The last key tile up to which the tiles from `a` on cost at most `budget`.
 int64_t span_end(const Tile& t, int64_t a, int64_t budget, int64_t suffix_weight) {
@@ -233,10 +234,10 @@ bool level_queues(const Costs& cm, const std::vector<Tile>& tiles, const std::ve
     for (const int32_t ti : owned[x]) {
       const int64_t c = tile_cost(cm, tiles[ti], wgt);
       if (heap.soonest() + c > level) {
-        left[x].push_back(Left{ti, 0});
+        left[x].push_back(Left{ti, tiles[ti].k0});
         continue;
       }
-      queues[x].push_back(Piece{ti, 0, tiles[ti].n_kt, heap.soonest()});
+      queues[x].push_back(Piece{ti, tiles[ti].k0, tiles[ti].n_kt, heap.soonest()});
       heap.take(c);
     }
     slots[x] = std::move(heap.s);
@@ -334,7 +335,8 @@ void level_plan(const Costs& cm, ExtendPlan& plan, const std::vector<Tile>& tile
   // (equal costs would not do: a full tile and a longer one of fewer rows may cost the same)
   std::vector<bool> as_before(X, false);
   auto shaped_alike = [&](int32_t a, int32_t c) {
-    return tiles[a].n_kt == tiles[c].n_kt && tiles[a].n_pre == tiles[c].n_pre && tiles[a].rows == tiles[c].rows;
+    return tiles[a].n_kt == tiles[c].n_kt && tiles[a].n_pre == tiles[c].n_pre && tiles[a].rows == tiles[c].rows &&
+           tiles[a].k0 == tiles[c].k0;
   };
   std::vector<int64_t> costs, last;
   int64_t ordered = 0, last_span = 0;
@@ -397,7 +399,7 @@ void level_plan(const Costs& cm, ExtendPlan& plan, const std::vector<Tile>& tile
     std::fill(n_of.begin(), n_of.end(), 1);
     pieces.assign(X, {});
     for (size_t x = 0; x < X; ++x)
-      for (const int32_t ti : owned[x]) pieces[x].push_back(Piece{ti, 0, tiles[ti].n_kt, 0});
+      for (const int32_t ti : owned[x]) pieces[x].push_back(Piece{ti, tiles[ti].k0, tiles[ti].n_kt, 0});
   }
   size_t n_groups = 0;
   for (const int32_t n : n_of) n_groups += n > 1 ? 1 : 0;
@@ -444,10 +446,10 @@ ExtendPlan build_extend_plan(const int32_t* prefix_lens, const int32_t* suffix_l
                              int32_t head_dim, int32_t block_m, int32_t wgs_per_cu,
                              int32_t num_cus, int32_t num_xcds, const Tuning& tuning,
                              const int32_t* cu_rows, const int32_t* bt_rows, int32_t maps,
-                             int64_t kv_bytes) {
+                             int64_t kv_bytes, const KeyLimits* limits) {
   ExtendPlan plan;
   plan.part_rows = block_m * maps;
-  plan.part_f32 = maps > 1;
+  plan.part_f32 = maps > 1 || limits != nullptr;
   plan.seqs.resize(num_seqs);
   int64_t cu = 0, n_tiles = 0;
   for (int32_t b = 0; b < num_seqs; ++b) {
@@ -469,11 +471,17 @@ ExtendPlan build_extend_plan(const int32_t* prefix_lens, const int32_t* suffix_l
       for (int64_t r0 = 0; r0 < rows; r0 += block_m) {
         const int32_t nr = static_cast<int32_t>(std::min<int64_t>(block_m, rows - r0));
         const int64_t t_last = (r0 + nr - 1) / gqa_group;
-        const int32_t kv_len = static_cast<int32_t>(prefix_lens[b] + t_last + 1);
+        int32_t kv_len = static_cast<int32_t>(prefix_lens[b] + t_last + 1), k0 = 0;
+        if (limits != nullptr) {
+          if (limits->full_lens != nullptr)
+            kv_len = std::max(kv_len, std::min(limits->full_lens[b], prefix_lens[b] + suffix_lens[b]));
+          const int64_t first = limits->window > 0 ? prefix_lens[b] + r0 / gqa_group + 1 - limits->window : 0;
+          k0 = static_cast<int32_t>(std::max<int64_t>(0, first) / BLOCK_N);
+        }
         const int32_t n_kt = (kv_len + BLOCK_N - 1) / BLOCK_N;
         tiles.push_back(Tile{b, h, static_cast<int32_t>(r0), nr, kv_len, n_kt,
-                             std::min(n_kt, prefix_lens[b] / BLOCK_N), maps > 1 ? 100 : row_rate(nr)});
-        total_kt += n_kt;
+                             std::min(n_kt, prefix_lens[b] / BLOCK_N), maps > 1 ? 100 : row_rate(nr), k0});
+        total_kt += n_kt - k0;
       }
     }
   }
@@ -511,7 +519,8 @@ ExtendPlan build_extend_plan(const int32_t* prefix_lens, const int32_t* suffix_l
     int64_t most = 1;
     for (int64_t ti = tb.first; ti < tb.first + tb.n; ++ti) {
       const Tile& t = tiles[ti];
-      const int64_t n_c = n_chunks(t.n_kt);
+      const int64_t n_kt = t.n_kt - t.k0;
+      const int64_t n_c = n_chunks(static_cast<int32_t>(n_kt));
       most = std::max(most, n_c);
       int32_t part0 = -1;
       if (n_c > 1) {
@@ -525,19 +534,21 @@ ExtendPlan build_extend_plan(const int32_t* prefix_lens, const int32_t* suffix_l
       // reaches past the cached prefix (read from the new tokens) counting
       // suffix_weight / 100 of a prefix tile (forced chunk sizes: equal key
       // counts); every chunk at least one tile long
-      const int64_t n_pre = t.n_pre;
+      const int64_t n_pre = std::max(0, t.n_pre - t.k0);
       const int64_t wgt = tuning.kv_chunk_tiles > 0 ? 100 : std::max(1, tuning.suffix_weight);
-      const int64_t total_cost = n_pre * 100 + (t.n_kt - n_pre) * wgt;
+      const int64_t total_cost = n_pre * 100 + (n_kt - n_pre) * wgt;
+      const size_t at0 = first.size();
       first.push_back(0);
       for (int64_t c = 1; c < n_c; ++c) {
-        int64_t b = c * t.n_kt / n_c;
+        int64_t b = c * n_kt / n_c;
         if (wgt != 100) {
           const int64_t goal = c * total_cost / n_c;
           b = goal <= n_pre * 100 ? (goal + 99) / 100 : n_pre + (goal - n_pre * 100 + wgt - 1) / wgt;
         }
-        first.push_back(std::min(std::max(b, first.back() + 1), t.n_kt - (n_c - c)));
+        first.push_back(std::min(std::max(b, first.back() + 1), n_kt - (n_c - c)));
       }
-      first.push_back(t.n_kt);
+      first.push_back(n_kt);
+      for (size_t i = at0; i < first.size(); ++i) first[i] += t.k0;
     }
     for (int64_t c = 0; c < most; ++c)
       for (int64_t i = 0; i < tb.n; ++i) {
@@ -733,7 +744,7 @@ ExtendPlan build_decode_plan(const int32_t* prefix_lens, int32_t num_seqs, int32
                              int32_t gqa_group, int32_t head_dim, int32_t page_size,
                              int32_t keys_per_tile, int32_t waves_per_cu, int32_t num_cus,
                              const Tuning& tuning, size_t meta_at, const int32_t* cu_rows,
-                             const int32_t* bt_rows, int32_t maps) {
+                             const int32_t* bt_rows, int32_t maps, bool part_f32) {
   ExtendPlan plan;
   plan.part_rows = gqa_group * maps;
   plan.seqs.resize(num_seqs);
@@ -800,7 +811,7 @@ ExtendPlan build_decode_plan(const int32_t* prefix_lens, int32_t num_seqs, int32
     return (a.kv_end - a.kv_begin) > (c.kv_end - c.kv_begin);
   });
   plan.items.insert(plan.items.end(), tails.begin(), tails.end());
-  plan.part_f32 = maps > 1 || chunk != plain_chunk;
+  plan.part_f32 = part_f32 || maps > 1 || chunk != plain_chunk;
   layout_workspace(plan, head_dim);
   plan.whole_meta_bytes = plan.meta_bytes;
   if (chunk != plain_chunk) {
