@@ -128,7 +128,7 @@ struct Geo {
   static constexpr int TILE = BLOCK_N * RB;          // bytes of one matrix's tile
   static constexpr int KT = D / 16;                  // k-steps of K Q^T
   static constexpr int DB = D / 32;                  // 32-row blocks of O^T
-    static constexpr int PRB = FP8 ? D : RB;           // bytes per pool row
+  static constexpr int PRB = FP8 ? D : RB;           // bytes per pool row
   static constexpr int B8 = D / 8;                   // fp8 bytes each lane stages per matrix
   static constexpr int KS = BLOCK_N / 16;            // fp8: key scales kept per tile, one per 16 keys
   static_assert(NI * RPI == 8, "each wave stages 8 rows of a tile");
@@ -301,32 +301,27 @@ void shaped_extend_kernel(ShapedParams sp, PlanArg<AP> ap) {
   };
   // fp8 pool rows into registers, values with their page's scale (`in_prefix`: the tile lies
   // wholly among cached keys from wg_lo on, so every row check passes)
-  struct Rows8 {
-    u32x4 x;
-    float s;
-  };
-  auto load8 = [&](int j0, int pg, const uint8_t* pool, uint32_t off, Rows8& rw, bool in_prefix,
+  auto load8 = [&](int j0, int pg, const uint8_t* pool, uint32_t off, u32x4& rw, bool in_prefix,
                    bool keys) __attribute__((always_inline)) {
     if (!in_prefix && !wanted(j0 + wrow0, 8)) return;
     const auto rs = rsrc_at(pool + size_t(pg) * page_stride);
-    if (!keys) rw.s = vs_s[size_t(pg) * hkv + kvh];
     const u32x2 a = __builtin_amdgcn_raw_buffer_load_b64(rs, off, 0, 0);
     if constexpr (T::B8 == 16) {
       const u32x2 b = __builtin_amdgcn_raw_buffer_load_b64(rs, (keys ? off ^ 64u : off) + 4 * D, 0, 0);
-      rw.x = u32x4{a.x, a.y, b.x, b.y};
+      rw = u32x4{a.x, a.y, b.x, b.y};
     } else {
-      rw.x = u32x4{a.x, a.y, 0u, 0u};
+      rw = u32x4{a.x, a.y, 0u, 0u};
     }
   };
   // `keys`: the codes are stored as they are
-  auto store8 = [&](int j0, const Rows8& rw, uint8_t* dst, bool in_prefix, bool keys) __attribute__((always_inline)) {
+  auto store8 = [&](int j0, const u32x4& rw, float s, uint8_t* dst, bool in_prefix, bool keys) __attribute__((always_inline)) {
     if (!in_prefix && !wanted(j0 + wrow0, 8)) return;
-    const PageScale sc = page_scale(rw.s);
+    const PageScale sc = page_scale(s);
     auto widen = [&](uint32_t a, uint32_t b) { return keys ? fp8x8_f16x8(a, b) : fp8x8_f16x8(a, b, sc); };
     auto ok = [&](int key) { return in_prefix || (key < lp && key >= wg_lo); };
-    if (ok(j0 + r8)) *reinterpret_cast<u32x4*>(dst + wrow0 * T::RB + 16 * lane) = widen(rw.x.x, rw.x.y);
+    if (ok(j0 + r8)) *reinterpret_cast<u32x4*>(dst + wrow0 * T::RB + 16 * lane) = widen(rw.x, rw.y);
     if constexpr (T::B8 == 16) {
-      if (ok(j0 + r8 + 4)) *reinterpret_cast<u32x4*>(dst + (wrow0 + 4) * T::RB + 16 * lane) = widen(rw.x.z, rw.x.w);
+      if (ok(j0 + r8 + 4)) *reinterpret_cast<u32x4*>(dst + (wrow0 + 4) * T::RB + 16 * lane) = widen(rw.z, rw.w);
     }
   };
   // fp8 pools: the new tokens' rows that this wave staged by DMA become fp16 in place
@@ -344,10 +339,22 @@ void shaped_extend_kernel(ShapedParams sp, PlanArg<AP> ap) {
     }
   };
 
-  // fp8 pools: page (then key scale) of the 16 keys from `key` on.  Behind the prefix or before
-  // what is visible: no page, scale unused.
-  auto scale_page = [&](int key) -> int { return wanted(key, 16) ? bt_s[key >> pshift] : 0; };
-  auto key_scale = [&](int key, int pg) -> float { return wanted(key, 16) ? ks_s[size_t(pg) * hkv + kvh] : 1.f; };
+  // fp8 pools.  In the loops pages and their scales come by vector loads, which have landed with the
+  // staging before them at the next iteration's barrier (by scalar loads the first LDS read of
+  // each iteration waited for them: 4096 tokens on 32768 keys at D = 64 3620 us, so 3340).  Each of a
+  // tile's groups of 16 keys lies in one page.  Iteration j takes, lane l, the page of group l % 4 of
+  // tile j + 4 (l < 4, whose rows are loaded next) or j + 3 (scales next), and the key (l < 8) or value
+  // scale of group l % 4 of tile j + 2.  Behind the prefix or before what is visible: no page, scale 1.
+  const int own = wave >> 1;  // the group of this wave's rows
+  auto pages_of = [&](int j0) __attribute__((always_inline)) -> int {
+    const int key = j0 + (lane < 4 ? 0 : BLOCK_N) + 16 * (lane & 3);
+    return wanted(key, 16) ? bt[key >> pshift] : 0;
+  };
+  auto scales_of = [&](int j0, int pg) __attribute__((always_inline)) -> float {
+    if (lane < 4 || !wanted(j0 + 16 * (lane & 3), 16)) return 1.f;
+    return (lane < 8 ? p.k_scale : p.v_scale)[size_t(pg) * hkv + kvh];
+  };
+  auto lane_of = [&](float v, int l) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), l)); };
 
   // ---- LDS fragment addresses (relative to a stage), as in the extend kernel: that of k-step kk
   // is k_addr ^ 32 kk, that of O^T block b is v_addr ^ 64 b (the swizzles are exclusive ors)
@@ -571,26 +578,28 @@ void shaped_extend_kernel(ShapedParams sp, PlanArg<AP> ap) {
   };
 
   // ---- prologue: the first tile's scores, its upper block's weights against their exact max
-  Rows8 k8{}, v8{};
+  u32x4 k8{}, v8{};
   int pg_k = 0, pg_v = 0;  // pages of the tiles to be issued (fp8: loaded) next
-  float ks_next[T::KS];    // fp8: key scales of the key tile of the next iteration, pages of the one after it
-  int pg_s[T::KS];
-#pragma unroll
-  for (int gi = 0; gi < T::KS; ++gi) {
-    ks_next[gi] = 1.f;
-    pg_s[gi] = 0;
-  }
-  // takes the key scales of iteration j's key tile and loads those of the next one's
-  auto next_scales = [&](int j, float (&ks)[T::KS], bool in_prefix) __attribute__((always_inline)) {
+  int pg_next = 0;         // page of the key tile after that (fp8: pages, of a lane each), on its way
+  float sc_next = 1.f;     // fp8: scales on their way
+  // At an iteration's start, what the one before has loaded: ks of the key tile, vs of the value rows to be
+  // stored.
+  auto arrive = [&](float (&ks)[T::KS], float& vs) __attribute__((always_inline)) {
+    pg_v = pg_k;
+    pg_k = FP8 ? __builtin_amdgcn_readlane(pg_next, own) : pg_next;
     if constexpr (FP8) {
 #pragma unroll
-      for (int gi = 0; gi < T::KS; ++gi) ks[gi] = ks_next[gi];
-#pragma unroll
-      for (int gi = 0; gi < T::KS; ++gi) {
-        if (in_prefix) ks_next[gi] = ks_s[size_t(pg_s[gi]) * hkv + kvh];
-        else ks_next[gi] = key_scale(tile0(j + 2) + 16 * gi, pg_s[gi]);
-        pg_s[gi] = in_prefix ? bt_s[(tile0(j + 3) + 16 * gi) >> pshift] : scale_page(tile0(j + 3) + 16 * gi);
-      }
+      for (int gi = 0; gi < T::KS; ++gi) ks[gi] = lane_of(sc_next, 4 + gi);
+      vs = lane_of(sc_next, 8 + own);
+    }
+  };
+  // ... and what iteration j loads for the next ones.
+  auto depart = [&](int j) __attribute__((always_inline)) {
+    if constexpr (FP8) {
+      sc_next = scales_of(tile0(j + 2), pg_next);
+      pg_next = pages_of(tile0(j + 4));
+    } else {
+      pg_next = load_page(tile0(j + 3));
     }
   };
   if (n_tiles > 0) {
@@ -599,35 +608,34 @@ void shaped_extend_kernel(ShapedParams sp, PlanArg<AP> ap) {
     issue(b0, lds_k0, pk0, true);
     issue(b0, lds_v0, pk0, false);
     if (n_tiles > 1) issue(tile0(1), lds_k1, pk1, true);
-    pg_k = load_page(tile0(2));
-    pg_v = pk1;
+    pg_k = pk1;
+    pg_next = FP8 ? pages_of(tile0(2)) : load_page(tile0(2));
     if constexpr (FP8) {
-      Rows8 ka{}, kb{}, va{};
+      u32x4 ka{}, kb{}, va{};
       load8(b0, pk0, k_pool, k8_off, ka, false, true);
       load8(b0, pk0, v_pool, v8_off, va, false, false);
       load8(tile0(1), pk1, k_pool, k8_off, kb, false, true);
+      const float vs0 = wanted(b0 + wrow0, 8) ? vs_s[size_t(pk0) * hkv + kvh] : 1.f;
       __builtin_amdgcn_s_waitcnt(0);
-      store8(b0, ka, lds_k0, false, true);
-      store8(b0, va, lds_v0, false, false);
-      store8(tile0(1), kb, lds_k1, false, true);
+      store8(b0, ka, 1.f, lds_k0, false, true);
+      store8(b0, va, vs0, lds_v0, false, false);
+      store8(tile0(1), kb, 1.f, lds_k1, false, true);
       convert_new(b0, lds_k0);
+      pg_k = __builtin_amdgcn_readlane(pg_next, own);
       load8(tile0(2), pg_k, k_pool, k8_off, k8, false, true);
-      load8(tile0(1), pg_v, v_pool, v8_off, v8, false, false);
-      pg_v = pg_k;
-      pg_k = load_page(tile0(3));
-#pragma unroll
-      for (int gi = 0; gi < T::KS; ++gi) {
-        const int key = tile0(1) + 16 * gi;
-        ks_next[gi] = key_scale(key, scale_page(key));
-        pg_s[gi] = scale_page(tile0(2) + 16 * gi);
-      }
+      load8(tile0(1), pk1, v_pool, v8_off, v8, false, false);
+      sc_next = scales_of(tile0(1), pg_next);
+      pg_next = pages_of(tile0(3));
     }
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
     if (wave_active) {
       float ks[T::KS], lsum;
 #pragma unroll
-      for (int gi = 0; gi < T::KS; ++gi) ks[gi] = FP8 ? key_scale(b0 + 16 * gi, scale_page(b0 + 16 * gi)) : 1.f;
+      for (int gi = 0; gi < T::KS; ++gi) {
+        const int key = b0 + 16 * gi;
+        ks[gi] = FP8 && wanted(key, 16) ? ks_s[size_t(bt_s[key >> pshift]) * hkv + kvh] : 1.f;
+      }
       f32x16 s[2];
       u32x4 kf[kSteps];
 #pragma unroll
@@ -657,12 +665,12 @@ void shaped_extend_kernel(ShapedParams sp, PlanArg<AP> ap) {
       convert_new(tile0(j), v_cur);
     }
     __syncthreads();  // everyone's has; the other stages are no longer read
-    float ks[T::KS] = {};
-    next_scales(j, ks, false);
+    float ks[T::KS] = {}, vs = 1.f;
+    arrive(ks, vs);
     if (j + 1 < n_tiles) {
       if constexpr (FP8) {
-        if (j + 2 < n_tiles) store8(tile0(j + 2), k8, k_nxt, false, true);
-        store8(tile0(j + 1), v8, v_nxt, false, false);
+        if (j + 2 < n_tiles) store8(tile0(j + 2), k8, 1.f, k_nxt, false, true);
+        store8(tile0(j + 1), v8, vs, v_nxt, false, false);
       }
       if (j + 2 < n_tiles) issue(tile0(j + 2), k_nxt, pg_k, true);
       issue(tile0(j + 1), v_nxt, pg_v, false);
@@ -670,8 +678,7 @@ void shaped_extend_kernel(ShapedParams sp, PlanArg<AP> ap) {
         load8(tile0(j + 3), pg_k, k_pool, k8_off, k8, false, true);
         load8(tile0(j + 2), pg_v, v_pool, v8_off, v8, false, false);
       }
-      pg_v = pg_k;
-      pg_k = load_page(tile0(j + (FP8 ? 4 : 3)));
+      depart(j);
     }
     // (also of tiles that no row of this wave sees: a branch around the phases made the compiler
     // copy O in every iteration)
@@ -689,8 +696,8 @@ void shaped_extend_kernel(ShapedParams sp, PlanArg<AP> ap) {
       convert_new(tile0(j), v_cur);
     }
     __syncthreads();
-    float ks[T::KS] = {};
-    next_scales(j, ks, !fresh);  // (new keys have none: for the loop behind this one, as the loads below)
+    float ks[T::KS] = {}, vs = 1.f;
+    arrive(ks, vs);
     if (!FP8 || fresh) {
       auto base = [&](int j0, int pg, const uint8_t* pool, const uint8_t* rows_new) {
         const ptrdiff_t row0 = ptrdiff_t(sq.cu) + j0 - lp;
@@ -705,14 +712,13 @@ void shaped_extend_kernel(ShapedParams sp, PlanArg<AP> ap) {
     }
     if constexpr (FP8) {
       if (!fresh) {
-        store8(tile0(j + 2), k8, k_nxt, true, true);
-        store8(tile0(j + 1), v8, v_nxt, true, false);
+        store8(tile0(j + 2), k8, 1.f, k_nxt, true, true);
+        store8(tile0(j + 1), v8, vs, v_nxt, true, false);
       }
       load8(tile0(j + 3), pg_k, k_pool, k8_off, k8, !fresh, true);
       load8(tile0(j + 2), pg_v, v_pool, v8_off, v8, !fresh, false);
     }
-    pg_v = pg_k;
-    pg_k = load_page(tile0(j + (FP8 ? 4 : 3)));
+    depart(j);
     if constexpr (decltype(rows)::value) phases(k_cur, v_cur, j, parity, std::integral_constant<Keys, Keys::kSeen>{}, false, ks);
   };
   // The ranges [begin, end) of iterations that may run so, new tokens and prefix.  Both: the keys of this
