@@ -32,10 +32,10 @@
 // fp8 rows are widened into LDS, values with their page's scale, key codes as they are (fp16 holds
 // them exactly): a key's page scale multiplies the scores in fp32.
 //
-// Bound by power without a cap (matrix cores busy some 60% of the cycles), with one by vector work
-// beside the products: per 16 scores of a lane 112 vector operations, 48 of them transcendental.  4096
-// tokens on 32768 keys, 32 query heads (2.34e12 operations): D = 128 2065 us (1130 TFLOP/s), cap
-// 2535, slopes 2130, fp8 2430; D = 64 2600, cap 3670, slopes 2520, fp8 3340.
+// Bound by power without a cap (matrix cores busy 61% of the cycles at 1.7 GHz), with one by vector
+// work beside the products (43% at 2.07): per 16 scores of a lane 112 vector operations, 48 of them
+// transcendental.  4096 tokens on 32768 keys, 32 query heads (2.34e12 operations): D = 128 2083 us
+// (1120 TFLOP/s), cap 2540, slopes 2119, fp8 2290; D = 64 2518, cap 3718, slopes 2491, fp8 3271.
 #pragma once
 
 #include <hip/hip_runtime.h>
