@@ -157,8 +157,8 @@ cw_status_t cw_residual_norm(const void* x, int64_t x_stride, const void* residu
  * attention of cw_step_attention without its page write: the pools are only read.
  *
  * Tensors, pools, scales, block table and lengths as for cw_extend_attention; out bf16 [T, Hq,
- * D], lse fp32 [T, Hq] or NULL; slopes device fp32 [Hq] of either sign, |slope (p - j)| below
- * 2^64; key_begins device int32 [T], any values; full_lens_h host int32 [num_seqs].  score_cap 0 or
+ * D], lse fp32 [T, Hq] or NULL; slopes device fp32 [Hq] of either sign, scores and |slope (p - j)|
+ * below 2^64; key_begins device int32 [T], any values; full_lens_h host int32 [num_seqs].  score_cap 0 or
  * 2^-10 .. 4096; a capped score is held to score_cap * 2^-20, a biased one to 2^-21 of the largest
  * score and bias of its row.  Block-table entries of pages that lie wholly before the windows of
  * all new tokens of their sequence are not read, nor is what those pages hold: a program may

@@ -322,19 +322,25 @@ __global__ __launch_bounds__(64) void shaped_decode_kernel(ShapedParams sp, Plan
     };
     weights();
     if (__any(!(tsum <= 0.5f * kSumLimit))) {
-      float f[16], mx = -INFINITY;
-      exponents(0.f, f);
+      float f[16];
+      auto largest = [&](float m) __attribute__((always_inline)) -> float {
+        exponents(m, f);
+        float mx = -INFINITY;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, f[i]);
-      mx = row_max(mx) - kHeadroom;
-      if (mx > m_run) {
-        const float alpha = __builtin_amdgcn_exp2f(m_run - mx);
-        m_run = mx;
-        l_run *= alpha;
+        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, f[i]);
+        return floorf(row_max(mx));
+      };
+      RunningMax rm(m_run, largest(0.f));
+      const float alpha = rm.settle(m_run, largest(rm.near));
+      l_run *= alpha;
 #pragma unroll
-        for (int b = 0; b < T::DB; ++b) o[b] *= alpha;
+      for (int b = 0; b < T::DB; ++b) o[b] *= alpha;
+      tsum = 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        w[i] = __builtin_amdgcn_exp2f(rm.exponent(f[i]));
+        tsum += w[i];
       }
-      weights();
     }
     l_run += tsum;
     // O^T += V^T P^T over the tile's two 16-key slices.  Neither form of the weights adds to the

@@ -452,6 +452,21 @@ void shaped_extend_kernel(ShapedParams sp, PlanArg<AP> ap) {
     if (masked && static_cast<uint32_t>(bk.at + n) >= seen) f = -INFINITY;
     return f;
   };
+  // Weights i - 1 and i (odd) in the operand type, and in the block's sums.
+  auto round_pair = [&](Block& bk, u32x4(&pf)[2], int i) __attribute__((always_inline)) {
+    float& l = i % 4 == 1 ? bk.la : bk.lb;
+    uint32_t two;
+    if constexpr (FP8) {
+      const f16x2 v = {static_cast<_Float16>(bk.w[i - 1]), static_cast<_Float16>(bk.w[i])};
+      l = __builtin_amdgcn_fdot2(v, f16x2{static_cast<_Float16>(1.f), static_cast<_Float16>(1.f)}, l, false);
+      two = as_u32(v);
+    } else {
+      const bf16x2 v = {static_cast<__bf16>(bk.w[i - 1]), static_cast<__bf16>(bk.w[i])};
+      l = __builtin_amdgcn_fdot2_f32_bf16(v, __builtin_bit_cast(bf16x2, 0x3F803F80u), l, false);
+      two = __builtin_bit_cast(uint32_t, v);
+    }
+    pf[i >> 3][(i & 7) >> 1] = two;
+  };
   auto unit = [&](Block& bk, const f32x16& x, const Scales& sc, bool masked, u32x4(&pf)[2], int t) __attribute__((always_inline)) {
 #pragma unroll
     for (int e = 0; e < kUnit; ++e) {
@@ -462,48 +477,31 @@ void shaped_extend_kernel(ShapedParams sp, PlanArg<AP> ap) {
       }
       const int i2 = (t - kDepth + 2) * kUnit + e, i3 = i2 - kUnit;
       if (i2 >= 0 && i2 < 16) bk.w[i2] = __builtin_amdgcn_exp2f(exponent_of(bk, x, sc, masked, m_run, i2));
-      if (i3 >= 0 && i3 < 16 && i3 % 2 == 1) {
-        float& l = i3 % 4 == 1 ? bk.la : bk.lb;
-        uint32_t two;
-        if constexpr (FP8) {
-          const f16x2 v = {static_cast<_Float16>(bk.w[i3 - 1]), static_cast<_Float16>(bk.w[i3])};
-          l = __builtin_amdgcn_fdot2(v, f16x2{static_cast<_Float16>(1.f), static_cast<_Float16>(1.f)}, l, false);
-          two = as_u32(v);
-        } else {
-          const bf16x2 v = {static_cast<__bf16>(bk.w[i3 - 1]), static_cast<__bf16>(bk.w[i3])};
-          l = __builtin_amdgcn_fdot2_f32_bf16(v, __builtin_bit_cast(bf16x2, 0x3F803F80u), l, false);
-          two = __builtin_bit_cast(uint32_t, v);
-        }
-        pf[i3 >> 3][(i3 & 7) >> 1] = two;
-      }
+      if (i3 >= 0 && i3 < 16 && i3 % 2 == 1) round_pair(bk, pf, i3);
     }
   };
-  auto weights = [&](const f32x16& x, const Scales& sc, int k0, bool masked, u32x4(&pf)[2], float& lsum) __attribute__((always_inline)) {
-    Block bk;
-    start(bk, k0, masked, m_run);
-#pragma unroll
-    for (int t = 0; t < kSteps + kLead; ++t) unit(bk, x, sc, masked, pf, t);
-    lsum = bk.la + bk.lb;
-  };
-  // The running max that a block's largest exponent calls for, a whole number.
-  auto block_max = [&](const f32x16& x, const Scales& sc, int k0, bool masked) __attribute__((always_inline)) -> float {
-    Block bk;
-    start(bk, k0, masked, 0.f);
-    float mx = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      if constexpr (CAP) bk.a[i] = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x[i] * (FP8 ? sc.g[i >> 3] : c)));
-      mx = fmaxf(mx, exponent_of(bk, x, sc, masked, 0.f, i));
-    }
-    return floorf(row_max(mx)) - kHeadroom;
-  };
-  // Weights of a block, with the running max raised where they are too large; `other`: weights of
-  // another block that O does not hold yet.
+  // Weights of a block, against the running max raised as far as they call for (RunningMax); `other`: weights
+  // of another block that O does not hold yet.
   auto raise = [&](const f32x16& x, const Scales& sc, int k0, bool masked, u32x4(&pf)[2], float& lsum,
                    u32x4* other) __attribute__((always_inline)) {
-    const float mx = fmaxf(block_max(x, sc, k0, masked), m_run);
-    const float alpha = __builtin_amdgcn_exp2f(m_run - mx);
-    m_run = mx;
+    Block bk;
+    float f[16];
+    if constexpr (CAP) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) bk.a[i] = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x[i] * (FP8 ? sc.g[i >> 3] : c)));
+    }
+    auto largest = [&](float m) __attribute__((always_inline)) -> float {  // the row's, rounded down
+      start(bk, k0, masked, m);
+      float mx = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        f[i] = exponent_of(bk, x, sc, masked, m, i);
+        mx = fmaxf(mx, f[i]);
+      }
+      return floorf(row_max(mx));
+    };
+    RunningMax rm(m_run, largest(0.f));
+    const float alpha = rm.settle(m_run, largest(rm.near));
     l_run *= alpha;
 #pragma unroll
     for (int b = 0; b < T::DB; ++b) o[b] *= alpha;
@@ -523,7 +521,12 @@ void shaped_extend_kernel(ShapedParams sp, PlanArg<AP> ap) {
         }
       }
     }
-    weights(x, sc, k0, masked, pf, lsum);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      bk.w[i] = __builtin_amdgcn_exp2f(rm.exponent(f[i]));
+      if (i % 2 == 1) round_pair(bk, pf, i);
+    }
+    lsum = bk.la + bk.lb;
   };
   // ---- state across iterations (of one parity, for the next of the other): the lower block's
   // scores of the tile in hand with their scales, its upper block's weights
@@ -649,9 +652,7 @@ void shaped_extend_kernel(ShapedParams sp, PlanArg<AP> ap) {
         s[i % 2] = mfma16<FP8>(kf[i], qf[i / 2], i > 1 ? s[i % 2] : f32x16{});
       }
       const Scales sc_up = block_scales(ks[2], ks[3], b0 + 32, Keys::kAny, s[1]);
-      const float mx = block_max(s[1], sc_up, b0 + 32, true);
-      if (mx > m_run) m_run = mx;
-      weights(s[1], sc_up, b0 + 32, true, p_up[0], lsum);
+      raise(s[1], sc_up, b0 + 32, true, p_up[0], lsum, nullptr);
       l_run = lsum;
       sc_low = block_scales(ks[0], ks[1], b0, Keys::kAny, s[0]);
       x_low[0] = s[0];
