@@ -168,11 +168,11 @@ cw_status_t cw_residual_norm(const void* x, int64_t x_stride, const void* residu
  * Sequences with one new token run on an HBM-streaming kernel, the others on a matrix-core
  * kernel, which over fp8 pools takes q, k_new, v_new and the cached values (code * scale) in
  * fp16: of such a call their magnitudes must lie below 65504 (and are held to 2^-25 where they
- * lie below 2^-14).  Key scales are applied to the scores in fp32 by both; a scale may be 0.
- * Values (code * scale) lie below 2^80.  A NaN or infinity in a value that some row of a chunk
- * sees may reach the rows of its sequence that do not (their weight for it is zero); what slots
- * at or past a prefix's end hold changes no result.  Lengths, plan, capture, aliasing and
- * errors as for cw_step_attention; the timing events are not recorded.  The plan depends on
+ * lie below 2^-14, beside 2^-11 of themselves where a V scale does not fit fp16's 11 bits).  Key
+ * scales are applied to the scores in fp32 by both; a scale may be 0.  Values (code * scale) lie
+ * below 2^80.  A NaN or infinity in a value that some row of a chunk sees may reach the rows of its
+ * sequence that do not (their weight for it is zero); what slots at or past a prefix's end hold
+ * changes no result.  Lengths, plan, capture, aliasing and errors as for cw_step_attention; the timing events are not recorded.  The plan depends on
  * window and full_lens_h, not on the other shapes.  Workspace: cw_shaped_workspace_bytes (0 if the
  * arguments are invalid). */
 size_t cw_shaped_workspace_bytes(const int32_t* prefix_lens_h, const int32_t* suffix_lens_h,
@@ -214,11 +214,11 @@ cw_status_t cw_shaped_attention(const void* q, const void* k_new, const void* v_
  * 1..512; out_scale finite, norm_eps finite and >= 0.  Sequences with one new token run on
  * the HBM-streaming kernel, the others on the matrix-core kernel, which over fp8 pools
  * takes q, k_new, v_new and the cached values (code * scale) in fp16: of such a call their
- * magnitudes must lie below 65504 (and are held to 2^-25 where they lie below 2^-14).  Key
- * scales are applied to the scores in fp32 by both.  The streaming kernel has no such limit:
- * V scales may differ as they like.  A scale may be 0 (a page of zeros).  Values (code *
- * scale) lie below 2^80, as they are summed in fp32 with weights of up to 2^16; with a norm,
- * mean(x_h^2) must be an fp32 number: values below about 2^59.  A NaN or infinity in a new token's value may
+ * magnitudes must lie below 65504 (and are held to 2^-25 where they lie below 2^-14, beside 2^-11
+ * of themselves where a V scale does not fit fp16's 11 bits).  Key scales are applied to the
+ * scores in fp32 by both.  The streaming kernel has no such limit: V scales may differ as they
+ * like.  A scale may be 0 (a page of zeros).  Values (code * scale) lie below 2^80, as they are
+ * summed in fp32 with weights of up to 2^16; with a norm, mean(x_h^2) must be an fp32 number: values below about 2^59.  A NaN or infinity in a new token's value may
  * reach the rows of earlier tokens of its sequence (their weight for it is zero); what slots at or
  * past a prefix's end hold changes no result.  Lengths, plan, capture, aliasing and errors as for
  * cw_step_attention; the timing events are not recorded.  Workspace:

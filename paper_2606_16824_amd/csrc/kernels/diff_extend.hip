@@ -72,16 +72,19 @@ __device__ __forceinline__ void dma16(__amdgpu_buffer_rsrc_t r, lds_void* dst, u
   __builtin_amdgcn_raw_ptr_buffer_load_lds(r, dst, 16, voff, soff, 0, 0);
 }
 
-// Page scale s = p2 x fm, p2 a power of two (applied exactly by the conversion), fm in
-// [1, 2) rounded to fp16.
+// Page scale s = p2 x fm: p2 a power of two (applied by the conversion), fm s's significand, rounded to fp16,
+// times a power of two of its own: of a scale in [2^-14, 2) all of it (p2 = 1), of a larger one 1, of a
+// smaller one 2^-14.  So what the conversion rounds, if anything (of scales below 2^-29), is multiplied with at
+// most 2^-13, and a value is rounded once, by the product, also where fp16 has fewer bits left for it.
 struct PageScale {
   float p2;
   f16x2 fm;
 };
 __device__ __forceinline__ PageScale page_scale(float s) {
   const uint32_t b = __float_as_uint(s);
-  const float p2 = __uint_as_float(b & 0x7F800000u);
-  const _Float16 m = static_cast<_Float16>(__uint_as_float((b & 0x807FFFFFu) | 0x3F800000u));
+  const uint32_t e = b & 0x7F800000u, em = min(max(e, 113u << 23), 127u << 23);
+  const float p2 = __uint_as_float(e - em + (127u << 23));
+  const _Float16 m = static_cast<_Float16>(__uint_as_float((b & 0x807FFFFFu) | em));
   return PageScale{p2, f16x2{m, m}};
 }
 template <bool HI>
