@@ -172,9 +172,9 @@ cw_status_t cw_residual_norm(const void* x, int64_t x_stride, const void* residu
  * scales are applied to the scores in fp32 by both; a scale may be 0.  Values (code * scale) lie
  * below 2^80.  A NaN or infinity in a value that some row of a chunk sees may reach the rows of its
  * sequence that do not (their weight for it is zero); what slots at or past a prefix's end hold
- * changes no result.  Lengths, plan, capture, aliasing and errors as for cw_step_attention; the timing events are not recorded.  The plan depends on
- * window and full_lens_h, not on the other shapes.  Workspace: cw_shaped_workspace_bytes (0 if the
- * arguments are invalid). */
+ * changes no result.  Lengths, plan, capture, aliasing and errors as for cw_step_attention; the
+ * timing events are not recorded.  The plan depends on window and full_lens_h, not on the other
+ * shapes.  Workspace: cw_shaped_workspace_bytes (0 if the arguments are invalid). */
 size_t cw_shaped_workspace_bytes(const int32_t* prefix_lens_h, const int32_t* suffix_lens_h,
                                  int32_t num_seqs, int32_t num_kv_heads, int32_t gqa_group,
                                  int32_t head_dim, int32_t page_size, cw_kv_dtype_t kv_dtype,
@@ -218,9 +218,10 @@ cw_status_t cw_shaped_attention(const void* q, const void* k_new, const void* v_
  * of themselves where a V scale does not fit fp16's 11 bits).  Key scales are applied to the
  * scores in fp32 by both.  The streaming kernel has no such limit: V scales may differ as they
  * like.  A scale may be 0 (a page of zeros).  Values (code * scale) lie below 2^80, as they are
- * summed in fp32 with weights of up to 2^16; with a norm, mean(x_h^2) must be an fp32 number: values below about 2^59.  A NaN or infinity in a new token's value may
- * reach the rows of earlier tokens of its sequence (their weight for it is zero); what slots at or
- * past a prefix's end hold changes no result.  Lengths, plan, capture, aliasing and errors as for
+ * summed in fp32 with weights of up to 2^16; with a norm, mean(x_h^2) must be an fp32 number:
+ * values below about 2^59.  A NaN or infinity in a new token's value may reach the rows of earlier
+ * tokens of its sequence (their weight for it is zero); what slots at or past a prefix's end hold
+ * changes no result.  Lengths, plan, capture, aliasing and errors as for
  * cw_step_attention; the timing events are not recorded.  Workspace:
  * cw_diff_workspace_bytes (0 if the arguments are invalid). */
 size_t cw_diff_workspace_bytes(const int32_t* prefix_lens_h, const int32_t* suffix_lens_h,

@@ -71,24 +71,24 @@ __device__ __forceinline__ float exponent(float s, float c, float cap2, float bi
 // How far a block raises a row's running max.  An exponent is held to some 2^-22 of the score and the bias
 // that are in it, which from about 2^26 on is more than kHeadroom: taken against the largest exponent as
 // it came out against m = 0, none need come out near 0, and the weights would overflow or all vanish.  So
-// that one gives the new max roughly (`near`), and the largest of the exponents against `near` is taken
-// out of them once more: the row's largest weight is then in [2^kHeadroom, 2^(kHeadroom + 1)) whatever was
-// rounded before.  What comes in is rounded down to whole numbers, and m stays one.  (A row that sees none
-// of the keys has -inf, and keeps its max.)
+// that one gives the new max roughly (`near`), and where the exponents against `near` are off, the largest of
+// them is taken out of them once more (`settle`): the row's largest weight is then in [2^kHeadroom,
+// 2^(kHeadroom + 1)) whatever was rounded before.  What comes in is rounded down to whole numbers, and m stays
+// one.  (A row that sees none of the keys has -inf, and keeps its max.)
 struct RunningMax {
   float near, from;
-  __device__ __forceinline__ RunningMax(float m_run, float top) : near(fmaxf(top - kHeadroom, m_run)), from(0.f) {}
-  // `top`: the largest exponent against `near`.  Raises m_run (it never falls) and returns the factor of
-  // what was summed against the old one.
-  __device__ __forceinline__ float settle(float& m_run, float top) {
-    from = fmaxf(top, m_run - near + kHeadroom);
+  __device__ __forceinline__ RunningMax(float m_run, float top) : near(fmaxf(top - kHeadroom, m_run)), from(kHeadroom) {}
+  // `top`: the largest exponent against `near`.  (The max never falls.)
+  __device__ __forceinline__ void settle(float m_run, float top) { from = fmaxf(top, m_run - near + kHeadroom); }
+  // An exponent against `near`, against the settled max.
+  __device__ __forceinline__ float exponent(float f) const { return f - from + kHeadroom; }
+  // Raises m_run and returns the factor of what was summed against the old one.
+  __device__ __forceinline__ float raise(float& m_run) const {
     const float m = fmaxf(near + (from - kHeadroom), m_run);
     const float alpha = __builtin_amdgcn_exp2f(m_run - m);
     m_run = m;
     return alpha;
   }
-  // An exponent against `near`, against the running max.
-  __device__ __forceinline__ float exponent(float f) const { return f - from + kHeadroom; }
 };
 
 }  // namespace shaped

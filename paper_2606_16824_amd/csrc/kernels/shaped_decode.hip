@@ -331,7 +331,8 @@ __global__ __launch_bounds__(64) void shaped_decode_kernel(ShapedParams sp, Plan
         return floorf(row_max(mx));
       };
       RunningMax rm(m_run, largest(0.f));
-      const float alpha = rm.settle(m_run, largest(rm.near));
+      rm.settle(m_run, largest(rm.near));
+      const float alpha = rm.raise(m_run);
       l_run *= alpha;
 #pragma unroll
       for (int b = 0; b < T::DB; ++b) o[b] *= alpha;

@@ -489,22 +489,41 @@ void shaped_extend_kernel(ShapedParams sp, PlanArg<AP> ap) {
                    u32x4* other) __attribute__((always_inline)) {
     Block bk;
     float f[16];
+    auto exponents = [&](float m) __attribute__((always_inline)) {
+      start(bk, k0, masked, m);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) f[i] = exponent_of(bk, x, sc, masked, m, i);
+    };
+    auto form = [&](bool settled, const RunningMax& rm) __attribute__((always_inline)) {
+      bk.la = bk.lb = 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        bk.w[i] = __builtin_amdgcn_exp2f(settled ? rm.exponent(f[i]) : f[i]);
+        if (i % 2 == 1) round_pair(bk, pf, i);
+      }
+      lsum = bk.la + bk.lb;
+    };
+    auto largest = [&]() __attribute__((always_inline)) -> float {
+      float mx = f[0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) mx = fmaxf(mx, f[i]);
+      return floorf(row_max(mx));
+    };
     if constexpr (CAP) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) bk.a[i] = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x[i] * (FP8 ? sc.g[i >> 3] : c)));
     }
-    auto largest = [&](float m) __attribute__((always_inline)) -> float {  // the row's, rounded down
-      start(bk, k0, masked, m);
-      float mx = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        f[i] = exponent_of(bk, x, sc, masked, m, i);
-        mx = fmaxf(mx, f[i]);
-      }
-      return floorf(row_max(mx));
-    };
-    RunningMax rm(m_run, largest(0.f));
-    const float alpha = rm.settle(m_run, largest(rm.near));
+    exponents(0.f);
+    RunningMax rm(m_run, largest());
+    exponents(rm.near);
+    form(false, rm);
+    // (a row whose max rises has a weight of 2^kHeadroom, if its exponents came out as they did against 0)
+    const bool off = !(lsum <= kSumLimit) || (rm.near > m_run && row_sum(lsum) < 64.f);
+    if (__builtin_expect(__any(off), 0)) {
+      rm.settle(m_run, largest());
+      form(true, rm);
+    }
+    const float alpha = rm.raise(m_run);
     l_run *= alpha;
 #pragma unroll
     for (int b = 0; b < T::DB; ++b) o[b] *= alpha;
@@ -524,12 +543,6 @@ void shaped_extend_kernel(ShapedParams sp, PlanArg<AP> ap) {
         }
       }
     }
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      bk.w[i] = __builtin_amdgcn_exp2f(rm.exponent(f[i]));
-      if (i % 2 == 1) round_pair(bk, pf, i);
-    }
-    lsum = bk.la + bk.lb;
   };
   // ---- state across iterations (of one parity, for the next of the other): the lower block's
   // scores of the tile in hand with their scales, its upper block's weights
