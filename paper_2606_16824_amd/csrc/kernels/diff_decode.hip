@@ -42,7 +42,8 @@ constexpr int kKeys = 32;             // keys of a tile
 // column's largest weight is at least 2^kHeadroom, its product at least 1, and what fp16 drops of
 // any other (2^-25) at most 2^-25 of that.  Further apart (one page's scale may be far above the
 // others', without any weight on it) they are pairs of bf16: 48 decodes of 2k-32k keys 329 -> 346
-// us at D = 128, 314 -> 326 at 64.
+// us at D = 128, 314 -> 326 at 64.  A scale of 0 is far from any other: all of the large weights may
+// be its page's, and the products that are left below 2^-25.
 constexpr float kNearScales = 256.f;
 
 // 16 bytes per lane from global memory straight into LDS (lane l at LDS address m0 + 16 l),
@@ -253,7 +254,7 @@ __global__ __launch_bounds__(64) void diff_decode_kernel(DiffParams dp, PlanArg<
       vs_max[m] = x;
 #pragma unroll
       for (int d = 1; d < 64; d <<= 1) vs_max[m] = fmaxf(vs_max[m], __shfl_xor(vs_max[m], d));
-      wide |= __any(x > 0.f && x * kNearScales < vs_max[m]);
+      wide |= __any(lane < n_pages && x * kNearScales < vs_max[m]);
     }
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
