@@ -16,7 +16,8 @@
 // the loads of kBatch heads of each lane before it uses them.  GPU time of one token (32 + 8 +
 // 8 heads of 128, bf16 pages) 3.6 us, of 16384 tokens 95 us (5.0 TB/s; a plain copy moves 4.9),
 // with fp8 pages 93, of 1531 tokens of 64 + 8 heads without pages 14.8 us.  With three axes a
-// lane's pairs of one axis are still read in 16-byte pieces: one token 4.6 us, 16384 tokens 95 us.
+// lane's pairs of one axis are still read in 16-byte pieces: one token 4.6 us, 16384 tokens 95 us (96 where
+// neighbouring pairs follow different axes and are read one by one).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

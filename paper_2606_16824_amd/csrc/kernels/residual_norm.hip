@@ -13,7 +13,9 @@
 // weights and a gate of all tokens in registers over the rows that it takes (read for each row
 // they would be as many bytes again as a row's).
 //
-// 16384 rows of 4096 bf16 elements: 0.54 GB in 105 us (5.1 TB/s); one row 3.2 us.
+// 16384 rows of 4096 bf16 elements: 0.54 GB in 105 us (5.1 TB/s); one row 3.2 us; an fp32 stream 155 us
+// (5.2), a gate for each token 131 (5.1).  Rows above 8192 elements hold 321 to 352 registers, one wave per
+// SIMD, so that no row's loads fly beside another's sums: 4096 rows of 16384 141 us (3.8 TB/s), fp32 173 (4.6).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

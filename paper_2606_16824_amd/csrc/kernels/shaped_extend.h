@@ -32,10 +32,12 @@
 // fp8 rows are widened into LDS, values with their page's scale, key codes as they are (fp16 holds
 // them exactly): a key's page scale multiplies the scores in fp32.
 //
-// Bound by power without a cap (matrix cores busy 61% of the cycles at 1.7 GHz), with one by vector
-// work beside the products (43% at 2.07): per 16 scores of a lane 112 vector operations, 48 of them
-// transcendental.  4096 tokens on 32768 keys, 32 query heads (2.34e12 operations): D = 128 2083 us
-// (1120 TFLOP/s), cap 2540, slopes 2119, fp8 2290; D = 64 2518, cap 3718, slopes 2491, fp8 3271.
+// Bound by power without a cap (matrix cores busy 61% of the cycles at 1.6 GHz), with one by vector
+// work beside the products (44% at 2.0): per 16 scores of a lane 112 vector operations, 48 of them
+// transcendental.  Short workgroups by their start: some 16 us each beside the tiles (one of 64 keys
+// 18.3 us, 32 of them 84).  4096 tokens on 32768 keys (2.34e12 operations: 32 query heads at D = 128, 64
+// at D = 64): D = 128 2040 us (1145 TFLOP/s), cap 2540, slopes 2120, fp8 2270 to 2500; D = 64 2560, cap 3700,
+// slopes 2550, fp8 2960.  fp8 instances of D = 128 with a cap or a bias spill 8 to 21 registers.
 #pragma once
 
 #include <hip/hip_runtime.h>
